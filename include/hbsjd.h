@@ -264,6 +264,149 @@ hbsjd_status hbsjd_bikl_rows(const float* logits_s, const float* logits_t, int64
                              int32_t V, float* out, void* stream);
 
 /*
+ * Operators on rows of logits around a distillation step: a teacher's answers in
+ * short form, the divergence from them with its gradient, and what is done to
+ * logits ahead of a draw. Unlike the calls above these are asynchronous: each
+ * queues its kernels on `stream` (a hipStream_t of the current device, NULL for
+ * its null stream) and returns, allocates nothing, keeps nothing and waits for
+ * nothing, so that it can be captured into a HIP graph; the buffers have to stay
+ * until the kernels have run. Any number of calls may be in flight at once on
+ * any streams, as long as none writes what another uses.
+ *
+ * A matrix of `rows` rows of V entries is given by its first entry, its element
+ * type and its row stride in entries (>= V; what lies between rows is neither
+ * read nor written). Rows may start at any element. V need not be a multiple of
+ * anything. All pointers are device memory of the current device.
+ *
+ * Data errors cannot be returned by a call that does not wait; they end up in
+ * the row they belong to, as NaN, and in no other row.
+ */
+typedef enum hbsjd_elem {
+    HBSJD_ELEM_F32 = 0,
+    HBSJD_ELEM_BF16 = 1,   /* upper half of an fp32 */
+    HBSJD_ELEM_F16 = 2     /* IEEE binary16 */
+} hbsjd_elem;
+
+#define HBSJD_ROWS_MAX_VOCAB 262144
+#define HBSJD_TOP_MAX 2048
+#define HBSJD_ADJUST_MAX_BIASES 1024
+
+/*
+ * A teacher's answer in short form: the K largest logits of every row.
+ *   values [rows][K]  fp32, in descending order, exactly the row's logits
+ *   index  [rows][K]  their entries; the lowest index first among equal logits
+ *   rest   [rows]     fp32, log of the sum over all other entries v of
+ *                     exp(logits[v] / temperature); -infinity when there are
+ *                     none or all are -infinity
+ * softmax(logits / temperature) at a listed entry is then
+ * exp(value / temperature) / (sum_k exp(value_k / temperature) + exp(rest)).
+ * -0 and +0 are equal. NaNs rank above +infinity, and a row that holds one has
+ * rest = NaN. 1 <= K <= min(V, HBSJD_TOP_MAX); temperature in [1e-6, 1e6];
+ * 1 <= V <= HBSJD_ROWS_MAX_VOCAB; 0 <= rows < 2^31. The outputs are contiguous
+ * and overlap neither each other nor the logits. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, int32_t elem,
+                                   int64_t ld, int32_t K, float temperature, float* values,
+                                   int32_t* index, float* rest, void* stream);
+
+/*
+ * Divergence of a student's rows from a teacher's short answers, with its
+ * gradient: the distillation loss of Sec. 3.1 (Eq. 3 with both weights 1/2) on
+ * the teacher's K listed entries and one class that holds all the others.
+ * With P = softmax over [values / temperature, rest], and q the student's
+ * softmax(logits / temperature), summed over the unlisted entries for the class
+ * of the others (q_0):
+ *   L_r  = forward_weight KL(P || q) + reverse_weight KL(q || P)
+ *   loss[r]    = w_r L_r
+ *   grad[r][v] = w_r dL_r / d logits[r][v]
+ * With K = V this is the divergence of the whole rows; with K < V it is a lower
+ * bound of it. Without `rest` P is the softmax over the listed entries alone
+ * and the others have no mass (then only the forward divergence is finite:
+ * reverse_weight has to be 0).
+ */
+typedef struct hbsjd_distill_args {
+    int64_t rows;             /* 0 <= rows < 2^31 */
+    int32_t V;                /* 1 <= V <= HBSJD_ROWS_MAX_VOCAB */
+    int32_t K;                /* 1 <= K <= HBSJD_TOP_MAX */
+    const void* logits;       /* the student's rows */
+    int64_t ld;
+    int32_t elem;             /* hbsjd_elem, of logits and grad */
+    float temperature;        /* in [1e-6, 1e6] */
+    const float* values;      /* [rows][K]: the teacher's logits, in any order */
+    const int32_t* index;     /* [rows][K]: their entries, none twice; -1: place not used */
+    const float* rest;        /* [rows] or NULL: log mass of the teacher's other entries at
+                                 this temperature */
+    float forward_weight;     /* both in [0, 1e6], not both 0 */
+    float reverse_weight;
+    const float* row_weight;  /* [rows] or NULL (1): w_r */
+} hbsjd_distill_args;
+
+/*
+ * loss: fp32 [rows] or NULL; grad: rows of args->elem with stride ld_grad, or
+ * NULL (not both NULL). grad may be the logits' buffer with the logits' stride,
+ * and overlaps no input otherwise. Probabilities below 2^-126 count as 0, and 0
+ * log 0 as 0. Called again with the loss's upstream gradient as row_weight it is
+ * the backward pass (a row is read once either way).
+ * A row with w_r = 0 is not read: its loss and gradient are 0. A row without a
+ * distribution (all of its logits or all of the teacher's answer -infinity or
+ * unused; a NaN or +infinity in either), with an index outside [0, V) other
+ * than -1, or with an index twice has NaN as its loss and all of its gradient; a
+ * row whose divergence is infinite (mass on an entry that the other side gives
+ * none) has the infinity as its loss and NaN in all of its gradient. Sums are
+ * held in fp32 and the gradient is rounded once. The same call gives the same
+ * bits. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* args, float* loss, void* grad,
+                                    int64_t ld_grad, void* stream);
+
+/*
+ * What is done to logits ahead of a draw (hbsjd_transform_rows takes the result
+ * as it is). For entry v of row r with logit x, in this order, each operation
+ * rounded once in fp32 and the result once to out's type:
+ *   c = how often v is among the row's tokens; if c > 0:
+ *       x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *       x = x - frequency[r] * c
+ *       x = x - presence[r]
+ *   x = x + the row's bias on v (the sum, in list order, of its entries for v)
+ *   x = -infinity where the row's mask does not allow v (whatever x is, NaN too)
+ * A part whose pointers are NULL is left out. Penalties are not checked; a
+ * repetition penalty is meant to be positive.
+ */
+typedef struct hbsjd_adjust_args {
+    int64_t rows;               /* 0 <= rows < 2^31 */
+    int32_t V;                  /* 1 <= V <= HBSJD_ROWS_MAX_VOCAB */
+    int32_t elem;               /* hbsjd_elem of the logits */
+    const void* logits;
+    int64_t ld;
+    const int32_t* tokens;      /* row r's list at tokens + r * ld_tokens (0: one list for all
+                                   rows); entries outside [0, V) are ignored */
+    int32_t n_tokens;           /* capacity of a list */
+    int64_t ld_tokens;          /* >= 0 */
+    const int32_t* token_count; /* [rows] entries used, clamped to [0, n_tokens], or NULL: all */
+    const float* repetition;    /* [rows] or NULL: 1 */
+    const float* presence;      /* [rows] or NULL: 0 */
+    const float* frequency;     /* [rows] or NULL: 0 */
+    const int32_t* bias_index;  /* row r's list at r * ld_bias (0: one list for all rows);
+                                   entries outside [0, V) are ignored */
+    const float* bias_value;    /* laid out alike */
+    int32_t n_bias;             /* <= HBSJD_ADJUST_MAX_BIASES */
+    int64_t ld_bias;            /* >= 0 */
+    const uint32_t* mask;       /* [n_masks][(V + 31) / 32] or NULL: bit v % 32 of word v / 32
+                                   set where entry v is allowed */
+    int32_t n_masks;
+    const int32_t* mask_row;    /* [rows] or NULL (row r has mask r): the row's mask, negative
+                                   for none; a row with one >= n_masks is NaN all over */
+} hbsjd_adjust_args;
+
+/*
+ * out: rows of V entries, fp32 or of the logits' type, stride ld_out. It may be
+ * the logits' buffer when type and stride are the logits', and overlaps no
+ * input otherwise. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_adjust_rows(const hbsjd_adjust_args* args, void* out, int32_t out_elem,
+                               int64_t ld_out, void* stream);
+
+/*
  * The distribution transform of the verifier rows (Sec. 4.2: the target p and
  * the reused proposals q are full-vocabulary distributions; guided logits under
  * CFG, "Independent progress") on caller-supplied logits, with the draw each

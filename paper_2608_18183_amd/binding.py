@@ -18,6 +18,7 @@ _lock = threading.Lock()
 _lib = None
 
 DTYPE_F32, DTYPE_BF16 = 0, 1
+ELEM_F32, ELEM_BF16, ELEM_F16 = 0, 1, 2
 EXEC_AUTO, EXEC_FULL, EXEC_COMPACT = 0, 1, 2
 VERIFY_PROB, VERIFY_GREEDY, VERIFY_AR, VERIFY_AR_GREEDY = 0, 1, 2, 3
 PROGRESS_INDEPENDENT, PROGRESS_SYNC = 0, 1
@@ -54,6 +55,22 @@ class _RolloutOut(ctypes.Structure):
                 ("mode_per_round", _P), ("stats", _P)]
 
 
+class _DistillArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("V", _I32), ("K", _I32), ("logits", _P),
+                ("ld", ctypes.c_int64), ("elem", _I32), ("temperature", ctypes.c_float),
+                ("values", _P), ("index", _P), ("rest", _P), ("forward_weight", ctypes.c_float),
+                ("reverse_weight", ctypes.c_float), ("row_weight", _P)]
+
+
+class _AdjustArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("V", _I32), ("elem", _I32), ("logits", _P),
+                ("ld", ctypes.c_int64), ("tokens", _P), ("n_tokens", _I32),
+                ("ld_tokens", ctypes.c_int64), ("token_count", _P), ("repetition", _P),
+                ("presence", _P), ("frequency", _P), ("bias_index", _P), ("bias_value", _P),
+                ("n_bias", _I32), ("ld_bias", ctypes.c_int64), ("mask", _P), ("n_masks", _I32),
+                ("mask_row", _P)]
+
+
 _SIGS = {
     "hbsjd_create": (_I32, [ctypes.POINTER(_ModelDesc), ctypes.c_uint64, _P, ctypes.POINTER(_P)]),
     "hbsjd_load_weights": (_I32, [_P, _P, ctypes.c_size_t]),
@@ -64,6 +81,10 @@ _SIGS = {
     "hbsjd_forward": (_I32, [_P, _I32, _P, _P, _P, _P]),
     "hbsjd_score_bikl": (_I32, [_P, _P, _I32, _P, _P, _P, _P, _P]),
     "hbsjd_bikl_rows": (_I32, [_P, _P, ctypes.c_int64, _I32, _P, _P]),
+    "hbsjd_top_logits_rows": (_I32, [ctypes.c_int64, _I32, _P, _I32, ctypes.c_int64, _I32,
+                                     ctypes.c_float, _P, _P, _P, _P]),
+    "hbsjd_distill_top_rows": (_I32, [ctypes.POINTER(_DistillArgs), _P, _P, ctypes.c_int64, _P]),
+    "hbsjd_adjust_rows": (_I32, [ctypes.POINTER(_AdjustArgs), _P, _I32, ctypes.c_int64, _P]),
     "hbsjd_verify_probs": (_I32, [_I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "hbsjd_transform_rows": (_I32, [_I32, _I32, _P, _I32, ctypes.c_float, _P, _I32,
                                     ctypes.c_uint64, _P, _P, _P, _P, _P]),
@@ -361,6 +382,227 @@ def hbsjd_bikl_rows(logits_s, logits_t, stream=None):
     L = load_library()
     _check(L.hbsjd_bikl_rows(_P(_dev_ptr(logits_s)), _P(_dev_ptr(logits_t)), rows, V,
                              _P(_dev_ptr(out)), _P(_stream_handle(stream))), "hbsjd_bikl_rows")
+    return out
+
+
+def _elem(dtype) -> int:
+    import torch
+    try:
+        return {torch.float32: ELEM_F32, torch.bfloat16: ELEM_BF16,
+                torch.float16: ELEM_F16}[dtype]
+    except KeyError:
+        raise ValueError(f"rows of logits are fp32, bf16 or fp16, not {dtype}") from None
+
+
+def _matrix(t, what: str, like=None):
+    """A device tensor [rows, V] whose rows are contiguous: its row stride."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{what}: expected a device tensor [rows, V]")
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError(f"{what}: expected shape {tuple(like.shape)} on {like.device}")
+    rows, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the entries of a row have to be adjacent")
+    if rows > 1 and t.stride(0) < V:
+        raise ValueError(f"{what}: rows overlap")
+    return t.stride(0) if rows > 1 else V
+
+
+def _vector(t, what: str, shape, dtype, device):
+    """A contiguous device tensor of this shape and type, or None."""
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor on {device}")
+    return t
+
+
+def _lists(t, what: str, rows: int, dtype, device):
+    """Lists of one length for every row, [rows, n], or [n] for all rows: their
+    length and row stride."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{what}: expected {dtype} on {device}")
+    if t.dim() not in (1, 2) or (t.dim() == 2 and t.shape[0] != rows):
+        raise ValueError(f"{what}: expected shape [{rows}, n] or [n]")
+    n = t.shape[-1]
+    if n > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the entries of a list have to be adjacent")
+    return n, t.stride(0) if t.dim() == 2 and rows > 1 else 0
+
+
+def _opt(t) -> _P:
+    return _P(None if t is None else t.data_ptr())
+
+
+class _OnStream:
+    """The device of `t` and a stream of it, for a call that does not wait:
+    outputs are allocated for that stream, and the caching allocator keeps the
+    inputs until it has run."""
+
+    def __init__(self, t, stream):
+        import torch
+        self._device = torch.cuda.device(t.device)
+        self._stream = None
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = (torch.cuda.ExternalStream(int(stream), device=t.device) if int(stream)
+                      else torch.cuda.default_stream(t.device))
+        if stream is not None:
+            if stream.device != t.device:
+                raise ValueError(f"the stream is on {stream.device}, the logits on {t.device}")
+            if stream != torch.cuda.current_stream(t.device):
+                self._stream = stream
+        self._handle = None if stream is None else stream.cuda_stream
+
+    def __enter__(self):
+        import torch
+        self._device.__enter__()
+        if self._stream is not None:
+            self._context = torch.cuda.stream(self._stream)
+            self._context.__enter__()
+        if self._handle is None:
+            self._handle = torch.cuda.current_stream().cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        if self._stream is not None:
+            self._context.__exit__(*exc)
+        self._device.__exit__(*exc)
+
+    def uses(self, *tensors) -> _P:
+        """The stream's handle, after noting that it uses these tensors."""
+        if self._stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._stream)
+        return _P(self._handle)
+
+
+def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None, out=None):
+    """logits: device tensor [rows, V], fp32, bf16 or fp16, with any row stride.
+    Returns device tensors (values fp32 [rows, k], index int32 [rows, k], rest
+    fp32 [rows]), written into `out` when given. Asynchronous on `stream` (the
+    current one by default), as are the two calls below."""
+    import torch
+    ld = _matrix(logits, "logits")
+    rows, V = logits.shape
+    k = int(k)
+    if k < 1:
+        raise ValueError("need k >= 1")
+    L = load_library()
+    with _OnStream(logits, stream) as on:
+        if out is None:
+            out = (torch.empty((rows, k), dtype=torch.float32, device=logits.device),
+                   torch.empty((rows, k), dtype=torch.int32, device=logits.device),
+                   torch.empty(rows, dtype=torch.float32, device=logits.device))
+        values = _vector(out[0], "values", (rows, k), torch.float32, logits.device)
+        index = _vector(out[1], "index", (rows, k), torch.int32, logits.device)
+        rest = _vector(out[2], "rest", (rows,), torch.float32, logits.device)
+        _check(L.hbsjd_top_logits_rows(rows, V, _opt(logits), _elem(logits.dtype), ld, k,
+                                       float(temperature), _opt(values), _opt(index), _opt(rest),
+                                       on.uses(logits, values, index, rest)),
+               "hbsjd_top_logits_rows")
+    return values, index, rest
+
+
+def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float = 1.0,
+                           forward_weight: float = 0.5, reverse_weight: float = 0.5,
+                           row_weight=None, grad=True, stream=None):
+    """logits: the student's rows, a device tensor [rows, V], fp32, bf16 or fp16,
+    with any row stride; values fp32 and index int32 [rows, K] and rest fp32
+    [rows] as hbsjd_top_logits_rows gives them for the teacher; row_weight fp32
+    [rows]. Returns (loss fp32 [rows], grad like logits). grad=False leaves the
+    gradient out (None), a tensor is written (the logits themselves too)."""
+    import torch
+    ld = _matrix(logits, "logits")
+    rows, V = logits.shape
+    dev = logits.device
+    if not isinstance(values, torch.Tensor) or values.dim() != 2:
+        raise ValueError(f"values: expected shape [{rows}, K]")
+    K = values.shape[1]
+    _vector(values, "values", (rows, K), torch.float32, dev)
+    if index is None:
+        raise ValueError("index: expected a tensor")
+    _vector(index, "index", (rows, K), torch.int32, dev)
+    _vector(rest, "rest", (rows,), torch.float32, dev)
+    _vector(row_weight, "row_weight", (rows,), torch.float32, dev)
+    L = load_library()
+    with _OnStream(logits, stream) as on:
+        loss = torch.empty(rows, dtype=torch.float32, device=dev)
+        if grad is True:
+            grad = torch.empty((rows, V), dtype=logits.dtype, device=dev)
+        elif grad is False:
+            grad = None
+        ld_grad = 0
+        if grad is not None:
+            ld_grad = _matrix(grad, "grad", logits)
+            if grad.dtype != logits.dtype:
+                raise ValueError("grad: expected the logits' type")
+        a = _DistillArgs(rows, V, K, _opt(logits), ld, _elem(logits.dtype), float(temperature),
+                         _opt(values), _opt(index), _opt(rest), float(forward_weight),
+                         float(reverse_weight), _opt(row_weight))
+        _check(L.hbsjd_distill_top_rows(
+            ctypes.byref(a), _opt(loss), _opt(grad), ld_grad,
+            on.uses(logits, values, index, rest, row_weight, loss, grad)),
+            "hbsjd_distill_top_rows")
+    return loss, grad
+
+
+def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, presence=None,
+                      frequency=None, bias_index=None, bias_value=None, mask=None, mask_row=None,
+                      out=None, out_dtype=None, stream=None):
+    """logits: device tensor [rows, V], fp32, bf16 or fp16, with any row stride.
+    tokens int32 [rows, n] (or [n] for all rows) with token_count int32 [rows];
+    repetition, presence and frequency fp32 [rows]; bias_index int32 and
+    bias_value fp32 [rows, n] (or [n]); mask int32 [masks, ceil(V / 32)], a bit
+    per allowed entry, with mask_row int32 [rows]. Returns the adjusted rows: a
+    new tensor of out_dtype (the logits' type by default; fp32 is what
+    hbsjd_transform_rows takes), or `out`, which may be the logits."""
+    import torch
+    ld = _matrix(logits, "logits")
+    rows, V = logits.shape
+    dev = logits.device
+    n_tokens = ld_tokens = n_bias = ld_bias = n_masks = 0
+    if tokens is not None:
+        n_tokens, ld_tokens = _lists(tokens, "tokens", rows, torch.int32, dev)
+    elif any(t is not None for t in (token_count, repetition, presence, frequency)):
+        raise ValueError("penalties without tokens")
+    if (bias_index is None) != (bias_value is None):
+        raise ValueError("bias_index and bias_value go together")
+    if bias_index is not None:
+        n_bias, ld_bias = _lists(bias_index, "bias_index", rows, torch.int32, dev)
+        if _lists(bias_value, "bias_value", rows, torch.float32, dev) != (n_bias, ld_bias):
+            raise ValueError("bias_index and bias_value have to be laid out alike")
+    if mask is not None:
+        n_masks = mask.shape[0]
+        _vector(mask, "mask", (n_masks, (V + 31) // 32), torch.int32, dev)
+        if n_masks == 0:
+            raise ValueError("mask: no masks")
+    for t, what, dtype in ((token_count, "token_count", torch.int32),
+                           (repetition, "repetition", torch.float32),
+                           (presence, "presence", torch.float32),
+                           (frequency, "frequency", torch.float32),
+                           (mask_row, "mask_row", torch.int32)):
+        _vector(t, what, (rows,), dtype, dev)
+    L = load_library()
+    with _OnStream(logits, stream) as on:
+        if out is None:
+            out = torch.empty((rows, V), dtype=out_dtype or logits.dtype, device=dev)
+        elif out_dtype is not None and out.dtype != out_dtype:
+            raise ValueError(f"out: expected {out_dtype}")
+        ld_out = _matrix(out, "out", logits)
+        a = _AdjustArgs(rows, V, _elem(logits.dtype), _opt(logits), ld, _opt(tokens), n_tokens,
+                        ld_tokens, _opt(token_count), _opt(repetition), _opt(presence),
+                        _opt(frequency), _opt(bias_index), _opt(bias_value), n_bias, ld_bias,
+                        _opt(mask), n_masks, _opt(mask_row))
+        _check(L.hbsjd_adjust_rows(
+            ctypes.byref(a), _opt(out), _elem(out.dtype), ld_out,
+            on.uses(logits, tokens, token_count, repetition, presence, frequency, bias_index,
+                    bias_value, mask, mask_row, out)), "hbsjd_adjust_rows")
     return out
 
 

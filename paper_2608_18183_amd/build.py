@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build", "obj")
 LIB = os.path.join(HERE, "libhbsjd.so")
-SOURCES = ["abi.hip", "gemm.hip", "attention.hip", "rowops.hip", "sampler.hip", "score.hip"]
+SOURCES = ["abi.hip", "gemm.hip", "attention.hip", "rowops.hip", "sampler.hip", "score.hip",
+           "abi_rows.hip", "toplogits.hip", "distill.hip", "adjust.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          # packed fp32 instructions stay off: some of their forms have given
          # wrong results on this hardware without any error

@@ -13,6 +13,7 @@
 #include "common.h"
 #include "launch.h"
 #include "round_graphs.h"
+#include "rows.h"
 
 #include <algorithm>
 #include <cmath>
@@ -47,6 +48,10 @@ struct DevBuf {
 };
 
 }  // namespace
+
+namespace hbsjd {
+hbsjd_status api_fail(hbsjd_status st, const std::string& msg) { return fail(st, msg); }
+}  // namespace hbsjd
 
 struct hbsjd_ctx {
     hbsjd_model_desc m{};
