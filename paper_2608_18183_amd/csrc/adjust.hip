@@ -14,14 +14,14 @@ namespace {
 constexpr int kPart = 4096;   // entries per workgroup
 
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void k_adjust(AdjustArgs a, int parts) {
+__global__ __launch_bounds__(256) void k_adjust(AdjustArgs a, int parts, int64_t item0) {
     constexpr int NT = 256;
     __shared__ int count[kPart];
     __shared__ float bias[kPart];
     __shared__ int list[HBSJD_ADJUST_MAX_BIASES];
     const int t = threadIdx.x;
-    const int64_t items = a.rows * parts;
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    {
+        const int64_t item = item0 + blockIdx.x;
         const int64_t r = item / parts;
         const int v0 = (int)(item - r * parts) * kPart, n = min(kPart, a.V - v0);
         const T* z = (const T*)a.logits + r * a.ld + v0;
@@ -82,7 +82,9 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustArgs a, int parts) {
 template <typename T, typename O>
 void go(const AdjustArgs& a, hipStream_t s) {
     const int parts = (a.V + kPart - 1) / kPart;
-    hipLaunchKernelGGL((k_adjust<T, O>), row_grid(a.rows * parts), dim3(256), 0, s, a, parts);
+    by_slabs(a.rows * parts, [&](int64_t item0, dim3 grid) {
+        hipLaunchKernelGGL((k_adjust<T, O>), grid, dim3(256), 0, s, a, parts, item0);
+    });
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "common.h"
 #include "hbsjd.h"
@@ -31,28 +32,152 @@ template <> __device__ __forceinline__ F16 narrow<F16>(float x) { return F16{f32
 
 inline size_t elem_size(int32_t elem) { return elem == HBSJD_ELEM_F32 ? 4 : 2; }
 
-// ------------------------------------------------------------ reductions
-// Block-wide reduction for blocks of NT threads in a fixed tree order; `red`
-// holds NT / 64 values. The caller puts a barrier before `red` is used again.
-template <int NT, typename F>
-__device__ __forceinline__ float block_all(float v, float* red, F op) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-    if constexpr (NT == 64) return v;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = red[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) r = op(r, red[w]);
-    return r;
-}
-struct MaxOp { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct AddOp { __device__ float operator()(float a, float b) const { return a + b; } };
+// ------------------------------------------------------------ 16-byte vectors
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// Rows are dealt to at most this many workgroups, which loop over them: a grid
-// of a workgroup a row would pass the 2^32 work items that a launch may have.
-constexpr int64_t kRowGrid = 1 << 20;
-inline dim3 row_grid(int64_t rows) { return dim3((unsigned)(rows < kRowGrid ? rows : kRowGrid)); }
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);   // entries per vector
+
+// vector j of a row: an unsigned byte offset from a base that is the same for the
+// whole wavefront takes one register, a 64-bit address two
+template <typename V> __device__ __forceinline__ V& vec_at(V* base, int j) {
+    return *(V*)((const char*)base + (uint32_t)j * 16u);
+}
+
+// a vector of -infinity
+template <typename T> __device__ __forceinline__ u32x4 masked_vec();
+template <> __device__ __forceinline__ u32x4 masked_vec<float>() { return 0xFF800000u; }
+template <> __device__ __forceinline__ u32x4 masked_vec<Bf16>() { return 0xFF80FF80u; }
+template <> __device__ __forceinline__ u32x4 masked_vec<F16>() { return 0xFC00FC00u; }
+
+// entry i of a vector; i is known at compile time wherever this is called
+template <typename T> __device__ __forceinline__ float vec_get(const u32x4& v, int i);
+template <> __device__ __forceinline__ float vec_get<float>(const u32x4& v, int i) {
+    return __uint_as_float(v[i]);
+}
+template <> __device__ __forceinline__ float vec_get<Bf16>(const u32x4& v, int i) {
+    return __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
+}
+template <> __device__ __forceinline__ float vec_get<F16>(const u32x4& v, int i) {
+    const uint32_t pair = v[i / 2];   // (a bit cast of the element itself reads the vector's first)
+    return (float)__builtin_bit_cast(f16x2, pair)[i & 1];
+}
+// -infinity into entry i where `on`
+template <typename T> __device__ __forceinline__ void vec_mask(u32x4& v, int i, bool on) {
+    if constexpr (sizeof(T) == 4) {
+        v[i] = on ? 0xFF800000u : v[i];
+    } else {
+        const uint32_t low = masked_vec<T>()[0] & 0xFFFFu;
+        v[i / 2] = !on ? v[i / 2] : i & 1 ? (v[i / 2] & 0xFFFFu) | low << 16 : (v[i / 2] & 0xFFFF0000u) | low;
+    }
+}
+// entries rounded to nearest even (the hardware's pair conversions)
+template <typename T> __device__ __forceinline__ u32x4 vec_pack(const float (&x)[kVec<T>]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __float_as_uint(x[i]);
+        } else {
+            const f32x2 p = {x[2 * i], x[2 * i + 1]};
+            if constexpr (std::is_same_v<T, Bf16>)
+                v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+            else
+                v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2));
+        }
+    }
+    return v;
+}
+
+// A row as 16-byte aligned vectors: up to kVec - 1 entries ahead of the first
+// one (a row may start at any entry) and as many behind the last, which single
+// threads hold ("edge" entries, numbered from 0: those ahead, then those
+// behind). Nothing outside the row is accessed, and rows of odd sizes and
+// strides move as whole vectors all the same.
+struct Span {
+    int head, vecs, tail;
+    template <typename T> __device__ __forceinline__ static Span of(const T* p, int V) {
+        Span s;
+        s.head = min(V, (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)));
+        s.vecs = (V - s.head) / kVec<T>;
+        s.tail = V - s.head - s.vecs * kVec<T>;
+        return s;
+    }
+    __device__ __forceinline__ int edges() const { return head + tail; }
+    // the entry of edge e
+    __device__ __forceinline__ int edge(int e, int V) const { return e < head ? e : V - tail + (e - head); }
+    // Entries in the order of the vectors, the edges behind them.
+    __device__ __forceinline__ int place(int v, int V) const {
+        return v < head ? V - head - tail + v : v < V - tail ? v - head : v;
+    }
+};
+
+// ------------------------------------------------------------ reductions
+// A wavefront's reduction, the same in every lane: DPP moves within the rows of
+// 16 lanes, then two row broadcasts (order fixed; a tenth of the latency of LDS
+// exchanges).
+template <int Ctrl, int RowMask> __device__ __forceinline__ float dpp_or(float v, float other) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(v), Ctrl,
+                                                      RowMask, 0xF, false));
+}
+struct MaxOp {
+    static constexpr float none = -INFINITY;
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct AddOp {
+    static constexpr float none = 0.f;
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+template <typename F> __device__ __forceinline__ float wave_all(float v, F op) {
+    v = op(v, dpp_or<0x111, 0xF>(v, F::none));   // row_shr 1, 2, 4, 8: lane 15 of a row has its row
+    v = op(v, dpp_or<0x112, 0xF>(v, F::none));
+    v = op(v, dpp_or<0x114, 0xF>(v, F::none));
+    v = op(v, dpp_or<0x118, 0xF>(v, F::none));
+    v = op(v, dpp_or<0x142, 0xA>(v, F::none));   // row_bcast 15 and 31: lane 63 has all
+    v = op(v, dpp_or<0x143, 0xC>(v, F::none));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// N block-wide reductions with one barrier, for blocks of NT threads. The caller
+// puts a barrier before the same `red` is used again.
+template <int NT, int N, typename F>
+__device__ __forceinline__ void block_all(float (&v)[N], float (*red)[NT / 64], F op) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_all(v[i], op);
+    if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[i][threadIdx.x >> 6] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float r[NT / 64];
+#pragma unroll
+            for (int w = 0; w < NT / 64; ++w) r[w] = red[i][w];
+#pragma unroll
+            for (int n = NT / 128; n > 0; n /= 2)
+#pragma unroll
+                for (int w = 0; w < n; ++w) r[w] = op(r[w], r[w + n]);
+            v[i] = r[0];
+        }
+    }
+}
+template <int NT, typename F> __device__ __forceinline__ float block_all(float v, float* red, F op) {
+    float a[1] = {v};
+    block_all<NT, 1>(a, (float (*)[NT / 64])red, op);
+    return a[0];
+}
+
+// Launches of a workgroup per item, in slabs: one launch of them all could pass
+// the 2^32 work items that a launch may have. (Workgroups that loop over items
+// hold whatever the compiler moves out of the loop: 96 registers and spills in
+// place of 81 in the divergence of fp32 rows of 16384.)
+template <typename F> inline void by_slabs(int64_t items, F f) {
+    constexpr int64_t kSlab = 1 << 21;
+    for (int64_t i0 = 0; i0 < items; i0 += kSlab)
+        f(i0, dim3((unsigned)(items - i0 < kSlab ? items - i0 : kSlab)));
+}
 
 // ------------------------------------------------------------ launchers
 struct TopArgs {

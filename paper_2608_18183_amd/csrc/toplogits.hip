@@ -20,14 +20,15 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_top(TopArgs a) {
+__global__ __launch_bounds__(256) void k_top(TopArgs a, int64_t r0) {
     constexpr int NT = 256;
     __shared__ uint64_t kept[HBSJD_TOP_MAX];
     __shared__ int hist[256];
     __shared__ int s_digit, s_above, s_n;
     __shared__ float red[NT / 64], red2[NT / 64];
     const int t = threadIdx.x;
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    {
+        const int64_t r = r0 + blockIdx.x;
         const T* z = (const T*)a.logits + r * a.ld;
         // the composite's upper 32 bits, then the 18 bits of the index
         uint64_t prefix = 0;
@@ -99,13 +100,15 @@ __global__ __launch_bounds__(256) void k_top(TopArgs a) {
 }  // namespace
 
 void top_logits(const TopArgs& a, hipStream_t s) {
-    const dim3 grid = row_grid(a.rows), block(256);
+    by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+    const dim3 block(256);
     if (a.elem == HBSJD_ELEM_F32)
-        hipLaunchKernelGGL(k_top<float>, grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_top<float>, grid, block, 0, s, a, r0);
     else if (a.elem == HBSJD_ELEM_BF16)
-        hipLaunchKernelGGL(k_top<Bf16>, grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_top<Bf16>, grid, block, 0, s, a, r0);
     else
-        hipLaunchKernelGGL(k_top<F16>, grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_top<F16>, grid, block, 0, s, a, r0);
+    });
 }
 
 }  // namespace hbsjd
