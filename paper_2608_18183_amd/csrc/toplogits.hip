@@ -2,113 +2,500 @@
 // equals), their indices, and the log mass of all other entries at temperature
 // tau: rest = log sum over the unlisted v of exp(z_v / tau).
 //
-// Logits are compared by an order-preserving 32-bit image. The K-th largest
-// image is found digit by digit from the top; among the entries equal to it the
-// lowest indices are taken, up to an index found the same way. The kept
-// entries are collected and sorted as 64-bit numbers, image above complemented
-// index, so no two are equal and the order of collection does not matter.
+// The row is read once and held in registers. Its K largest entries are found
+// in three steps:
+//   1. A pivot p0 that at least K entries reach. The row is cut into groups
+//      (a thread's entries, or an eighth of them for large K), each wavefront
+//      takes the ceil(K / wavefronts)-th largest of its groups' maxima, and p0 is
+//      the least of these: as many different entries as groups reach it.
+//      Sampling maxima this way leaves 1.3 to 2 K candidates of ordinary rows.
+//   2. The entries that reach p0 are collected as 64-bit numbers, an
+//      order-preserving image of the logit above the complemented index, so no
+//      two are equal. The mass below p0 is summed in the same pass.
+//   3. A candidate's place in the output is the number of larger ones: counted
+//      over all of them when they are few, else over those of its bin, in bins
+//      of equal width between the least and the largest candidate.
+// Rows on which this fails (more candidates or equal ones than there is room
+// for, fewer than K entries above -infinity, NaN) take digit-by-digit selection
+// and a bitonic sort instead, with the same results.
 #include "rows.h"
 
 namespace hbsjd {
 namespace {
 
+constexpr int kBins = 1024;
+constexpr int kPairs = 256;      // candidates compared with all others
+constexpr int kBinMost = 256;    // entries of one bin
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
 // larger for larger logits; -0 as +0, every NaN above +infinity
 __device__ __forceinline__ uint32_t order_of(float x) {
-    uint32_t u = __float_as_uint(x + 0.f);
-    if (x != x) return 0xFFFFFFFFu;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(x + 0.f);
+    const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return x != x ? 0xFFFFFFFFu : k;
 }
+__device__ __forceinline__ float value_of(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+__device__ __forceinline__ uint64_t ranked(float x, int v) {
+    return (uint64_t)order_of(x) << 32 | (uint32_t)~v;
+}
+__device__ __forceinline__ int index_of(uint64_t c) { return (int)~(uint32_t)c; }
+__device__ __forceinline__ float logit_of(uint64_t c) { return value_of((uint32_t)(c >> 32)); }
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_top(TopArgs a, int64_t r0) {
-    constexpr int NT = 256;
-    __shared__ uint64_t kept[HBSJD_TOP_MAX];
-    __shared__ int hist[256];
-    __shared__ int s_digit, s_above, s_n;
-    __shared__ float red[NT / 64], red2[NT / 64];
+// room for candidates
+inline int top_cap(int K) { return K <= 256 ? 1024 : 4096; }
+inline size_t top_lds(int cap) { return (size_t)cap * 10 + (kBins + 1) * 4; }
+
+// Where a row's entries come from and its results go: a row of logits, or the
+// lists of a row's parts, whose entry v stands for entry map[v] and to whose
+// rest the parts' rests are added.
+struct TopRow {
+    float* values;
+    int32_t* index;
+    float* rest;
+    const int32_t* map;
+    const float* rests;
+    int n_rests;
+    int first;   // of the row's entries in the whole row
+    __device__ __forceinline__ void put(int k, uint64_t c) const {
+        values[k] = logit_of(c);
+        index[k] = map ? map[index_of(c)] : first + index_of(c);
+    }
+    // rest from the log of what the kernel itself left over
+    __device__ __forceinline__ void put_rest(float own) const {
+        float m = own;
+        for (int i = 0; i < n_rests; ++i) m = fmaxf(m, rests[i]);
+        if (n_rests && own == own && fabsf(m) != INFINITY) {
+            float s = __expf(own - m);
+            for (int i = 0; i < n_rests; ++i) s += __expf(rests[i] - m);
+            own = m + __logf(s);
+        } else if (n_rests && own == own) {
+            own = m;
+        }
+        *rest = own;
+    }
+};
+
+// the digits' way, from memory, for rows of any kind
+template <int NT, typename T>
+__device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const TopRow& out,
+                              uint64_t* kept, int* hist, float* red, int* word) {
     const int t = threadIdx.x;
-    {
-        const int64_t r = r0 + blockIdx.x;
-        const T* z = (const T*)a.logits + r * a.ld;
-        // the composite's upper 32 bits, then the 18 bits of the index
-        uint64_t prefix = 0;
-        int need = a.K;   // rank of the wanted entry among those that share the prefix
-        for (int shift = 48; shift >= 0; shift -= 8) {
-            __syncthreads();
-            hist[t] = 0;
-            __syncthreads();
-            for (int v = t; v < a.V; v += NT) {
-                const uint64_t c = (uint64_t)order_of(widen(z[v])) << 24 | (0xFFFFFFu - v);
-                if (shift == 48 || c >> (shift + 8) == prefix) atomicAdd(&hist[c >> shift & 255], 1);
-            }
-            __syncthreads();
-            if (t == 0) {
-                int above = 0, d = 255;
-                while (above + hist[d] < need) above += hist[d--];
-                s_digit = d;
-                s_above = above;
-            }
-            __syncthreads();
-            prefix = prefix << 8 | s_digit;
-            need -= s_above;
-        }
-        if (t == 0) s_n = 0;
+    uint64_t prefix = 0;
+    int need = K;   // rank of the wanted entry among those that share the prefix
+    for (int shift = 56; shift >= 0; shift -= 8) {
         __syncthreads();
-        float m = -INFINITY;
-        for (int v = t; v < a.V; v += NT) {
-            const float x = widen(z[v]);
-            const uint64_t c = (uint64_t)order_of(x) << 24 | (0xFFFFFFu - v);
-            if (c >= prefix) kept[atomicAdd(&s_n, 1)] = c;
-            else m = fmaxf(m, x);
+        for (int i = t; i < 256; i += NT) hist[i] = 0;
+        __syncthreads();
+        for (int v = t; v < V; v += NT) {
+            const uint64_t c = ranked(widen(z[v]), v);
+            if (shift == 56 || c >> (shift + 8) == prefix) atomicAdd(&hist[c >> shift & 255], 1);
         }
-        int n = 1;
-        while (n < a.K) n *= 2;
-        for (int i = a.K + t; i < n; i += NT) kept[i] = 0;
-        m = block_all<NT>(m, red, MaxOp());
-        float s = 0.f;
-        for (int v = t; v < a.V; v += NT) {
-            const float x = widen(z[v]);
-            const uint64_t c = (uint64_t)order_of(x) << 24 | (0xFFFFFFu - v);
-            if (c < prefix) s += __expf((x - m) * a.inv_tau);
+        __syncthreads();
+        if (t == 0) {
+            int above = 0, d = 255;
+            while (d > 0 && above + hist[d] < need) above += hist[d--];
+            word[0] = d;
+            word[1] = above;
         }
-        s = block_all<NT>(s, red2, AddOp());
-        for (int size = 2; size <= n; size *= 2)
-            for (int step = size / 2; step > 0; step /= 2) {
-                __syncthreads();
-                for (int i = t; i < n / 2; i += NT) {
-                    const int lo = (i / step) * 2 * step + i % step, hi = lo + step;
-                    const uint64_t x = kept[lo], y = kept[hi];
-                    if ((x < y) == !(lo & size)) {
-                        kept[lo] = y;
-                        kept[hi] = x;
-                    }
+        __syncthreads();
+        prefix = prefix << 8 | word[0];
+        need -= word[1];
+    }
+    if (t == 0) word[2] = 0;
+    __syncthreads();
+    float m = -INFINITY;
+    for (int v = t; v < V; v += NT) {
+        const float x = widen(z[v]);
+        const uint64_t c = ranked(x, v);
+        if (c >= prefix) kept[atomicAdd(&word[2], 1)] = c;
+        else m = fmaxf(m, x);
+    }
+    int n = 1;
+    while (n < K) n *= 2;
+    for (int i = K + t; i < n; i += NT) kept[i] = 0;
+    m = block_all<NT>(m, red, MaxOp());
+    float s = 0.f;
+    for (int v = t; v < V; v += NT) {
+        const float x = widen(z[v]);
+        if (ranked(x, v) < prefix) s += __expf((x - m) * inv_tau);
+    }
+    __syncthreads();
+    s = block_all<NT>(s, red, AddOp());
+    for (int size = 2; size <= n; size *= 2)
+        for (int step = size / 2; step > 0; step /= 2) {
+            __syncthreads();
+            for (int i = t; i < n / 2; i += NT) {
+                const int lo = (i / step) * 2 * step + i % step, hi = lo + step;
+                const uint64_t x = kept[lo], y = kept[hi];
+                if ((x < y) == !(lo & size)) {
+                    kept[lo] = y;
+                    kept[hi] = x;
                 }
             }
-        __syncthreads();
-        for (int k = t; k < a.K; k += NT) {
-            const int v = 0xFFFFFF - (int)(kept[k] & 0xFFFFFF);
-            a.values[r * a.K + k] = widen(z[v]);
-            a.index[r * a.K + k] = v;
         }
-        if (t == 0) {
-            const bool nan = kept[0] >> 24 == 0xFFFFFFFFu;
-            a.rest[r] = nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * a.inv_tau + __logf(s);
+    __syncthreads();
+    for (int k = t; k < K; k += NT) out.put(k, kept[k]);
+    if (t == 0) {
+        const bool nan = kept[0] >> 32 == 0xFFFFFFFFu;
+        out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s));
+    }
+}
+
+// exclusive prefix sum over a wavefront's lanes, and the wavefront's total
+__device__ __forceinline__ int wave_prefix(int v, int& total) {
+    int s = v;
+    auto step = [&](int moved) { s += moved; };
+    step(__builtin_amdgcn_update_dpp(0, s, 0x111, 0xF, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, s, 0x112, 0xF, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, s, 0x114, 0xF, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, s, 0x118, 0xF, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, s, 0x142, 0xA, 0xF, false));
+    step(__builtin_amdgcn_update_dpp(0, s, 0x143, 0xC, 0xF, false));
+    total = __builtin_amdgcn_readlane(s, 63);
+    return s - v;
+}
+
+// keeps the compiler from holding what one pass made of the vectors (the widened
+// entries of 16-bit rows, twice their registers) for the next
+template <int NV> __device__ __forceinline__ void opaque(u32x4 (&x)[NV]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
+}
+
+template <typename T, int NT, int NV>
+__device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out,
+                                        int cap) {
+    constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
+    static_assert(N >= 8, "eight groups a thread");
+    extern __shared__ uint64_t cand[];
+    int* bins = (int*)(cand + cap);
+    uint16_t* perm = (uint16_t*)(bins + kBins + 1);
+    __shared__ float red[4][NW];
+    __shared__ int s_count[NW];
+    __shared__ int word[4];
+    __shared__ float s_last;
+    const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
+    const float c2 = inv_tau * kLog2e;
+
+    const Span sp = Span::of(z, V);
+    const u32x4* z4 = (const u32x4*)(z + sp.head);
+    u32x4 x[NV];
+    float xe = -INFINITY;
+    if (sp.vecs > 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min(t + NT * i, sp.vecs - 1));
+    if (t < sp.edges()) xe = widen(z[sp.edge(t, V)]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (t + NT * i >= sp.vecs) x[i] = masked_vec<T>();
+
+    // ---- 1. the pivot
+    float p0 = -INFINITY;
+    const bool sample = NT * 8 >= 2 * K;
+    if (sample) {
+        float g[8];
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int n = b * N / 8; n < (b + 1) * N / 8; ++n) m = fmaxf(m, vec_get<T>(x[n / E], n % E));
+            g[b] = m;
+        }
+        int groups = 8;
+#pragma unroll
+        for (int h = 4; h > 0; h /= 2)
+            if (groups == 2 * h && NT * h >= 2 * K) {
+#pragma unroll
+                for (int b = 0; b < h; ++b) g[b] = fmaxf(g[b], g[b + h]);
+                groups = h;
+            }
+        const int want = (K + NW - 1) / NW;
+        uint32_t pivot = 0;
+        // the upper 24 bits will do: a lower pivot is a pivot too
+        auto descend = [&](auto n) {
+            uint32_t key[decltype(n)::value];
+#pragma unroll
+            for (int b = 0; b < decltype(n)::value; ++b) key[b] = order_of(g[b]);
+            for (int bit = 31; bit >= 8; --bit) {
+                const uint32_t next = pivot | 1u << bit;
+                int have = 0;
+#pragma unroll
+                for (int b = 0; b < decltype(n)::value; ++b) have += __popcll(__ballot(key[b] >= next));
+                if (have >= want) pivot = next;
+            }
+        };
+        if (groups == 1) descend(std::integral_constant<int, 1>{});
+        else if (groups == 2) descend(std::integral_constant<int, 2>{});
+        else if (groups == 4) descend(std::integral_constant<int, 4>{});
+        else descend(std::integral_constant<int, 8>{});
+        p0 = pivot > 0x007FFFFFu ? value_of(pivot) : -INFINITY;
+        if (NW > 1) {
+            if (lane == 0) red[0][wv] = p0;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NW; ++w) p0 = fminf(p0, red[0][w]);
         }
     }
+    // -infinity is nobody's candidate
+    const float from = fmaxf(p0, -3.4028234663852886e38f);
+    const float ref = p0 == -INFINITY ? 0.f : p0;
+
+    // ---- 2. candidates, and the mass below them
+    opaque(x);
+    int mine = 0;
+    float below = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            const float y = vec_get<T>(x[i], q);
+            const bool in = y >= from;
+            const float e = __builtin_amdgcn_exp2f((y - ref) * c2);
+            mine += in;
+            below += in ? 0.f : e;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    {
+        const bool in = xe >= from;
+        mine += in;
+        below += in ? 0.f : __builtin_amdgcn_exp2f((xe - ref) * c2);
+    }
+    int total;
+    int slot = wave_prefix(mine, total);
+    below = wave_all(below, AddOp());
+    if (lane == 0) {
+        s_count[wv] = total;
+        red[1][wv] = below;
+    }
+    __syncthreads();
+    int C = 0;
+    below = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < wv) slot += s_count[w];
+        C += s_count[w];
+        below += red[1][w];
+    }
+    if (C > cap || C < K || below != below) {
+        __syncthreads();
+        top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+        return;
+    }
+    opaque(x);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            const float y = vec_get<T>(x[i], q);
+            if (y >= from) cand[slot++] = ranked(y, sp.head + (t + NT * i) * E + q);
+        }
+    }
+    if (xe >= from) cand[slot++] = ranked(xe, sp.edge(t, V));
+
+    // ---- 3. places
+    if (C <= kPairs) {
+        __syncthreads();
+        for (int c = t; c < C; c += NT) {
+            const uint64_t me = cand[c];
+            int place = 0;
+            for (int j = 0; j < C; ++j) place += cand[j] > me;
+            if (place < K) out.put(place, me);
+            if (place == K - 1) s_last = logit_of(me);
+            perm[c] = place;
+        }
+        __syncthreads();
+    } else {
+        for (int i = t; i <= kBins; i += NT) bins[i] = 0;
+        if (t == 0) {
+            word[0] = -1;   // as unsigned: least image
+            word[1] = 0;    // largest
+            word[2] = 0;    // most entries in a bin
+        }
+        __syncthreads();
+        uint32_t least = 0xFFFFFFFFu, most = 0;
+        for (int c = t; c < C; c += NT) {
+            const uint32_t k = cand[c] >> 32;
+            least = min(least, k);
+            most = max(most, k);
+        }
+        atomicMin((uint32_t*)&word[0], least);
+        atomicMax((uint32_t*)&word[1], most);
+        __syncthreads();
+        least = word[0];
+        most = word[1];
+        const float lo = value_of(least), hi = value_of(most);
+        // Bins on the images where all candidates have one sign: even an outlier
+        // among them only costs some octaves. Across zero, where the images of
+        // small numbers would take most bins, on the logits themselves.
+        const bool images = (least ^ most) >> 31 == 0 || !(hi - lo < INFINITY);
+        const int shift = max(22 - __clz((int)(most - least)), 0);
+        const float scale = (kBins - 1) / (hi - lo);
+        auto bin_of = [&](uint64_t c) {
+            const uint32_t k = c >> 32;
+            // from the largest down
+            const int b = images ? (int)((k - least) >> shift) : (int)((value_of(k) - lo) * scale);
+            return kBins - 1 - min(max(b, 0), kBins - 1);
+        };
+        for (int c = t; c < C; c += NT) atomicAdd(&bins[bin_of(cand[c])], 1);
+        __syncthreads();
+        // exclusive prefix sums: thread t has its consecutive bins
+        constexpr int B = kBins / NT > 0 ? kBins / NT : 1;
+        int own[B], sum = 0, big = 0;
+        if (t * B < kBins)
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                own[b] = bins[t * B + b];
+                sum += own[b];
+                big = max(big, own[b]);
+            }
+        int all;
+        int start = wave_prefix(sum, all);
+        if (lane == 0) s_count[wv] = all;
+        atomicMax(&word[2], big);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (w < wv) start += s_count[w];
+        if (word[2] > kBinMost) {
+            __syncthreads();
+            top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+            return;
+        }
+        if (t * B < kBins)
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                bins[t * B + b] = start;
+                start += own[b];
+            }
+        __syncthreads();
+        // candidates by bin; afterwards bins[b] is where bin b + 1 starts
+        for (int c = t; c < C; c += NT) perm[atomicAdd(&bins[bin_of(cand[c])], 1)] = c;
+        __syncthreads();
+        for (int c = t; c < C; c += NT) {
+            const uint64_t me = cand[c];
+            const int b = bin_of(me), from_ = b ? bins[b - 1] : 0, to = bins[b];
+            if (from_ >= K) continue;
+            int place = from_;
+            for (int j = from_; j < to; ++j) place += cand[perm[j]] > me;
+            if (place < K) out.put(place, me);
+            if (place == K - 1) s_last = logit_of(me);
+        }
+        __syncthreads();
+    }
+
+    // ---- the mass of the others: below the pivot, and the candidates left over
+    const float last = s_last;
+    const uint32_t last_image = order_of(last);
+    if (last == INFINITY && C > K) {
+        __syncthreads();
+        top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+        return;
+    }
+    float over = 0.f;
+    if (C > K) {
+        // those whose place is K or more, in the order of the list
+        if (C <= kPairs) {
+            for (int c = t; c < C; c += NT)
+                if (perm[c] >= K) over += __builtin_amdgcn_exp2f((logit_of(cand[c]) - last) * c2);
+        } else {
+            // equal ones count the same whichever of them were taken
+            int taken = 0;
+            for (int c = t; c < C; c += NT) {
+                const uint32_t k = cand[c] >> 32;
+                if (k < last_image) over += __builtin_amdgcn_exp2f((value_of(k) - last) * c2);
+                taken += k >= last_image;
+            }
+            int n;
+            wave_prefix(taken, n);
+            if (lane == 0) s_count[wv] = n;
+        }
+        float o[1] = {over};
+        block_all<NT, 1>(o, &red[2], AddOp());
+        over = o[0];
+        if (C > kPairs) {
+            if (NT == 64) __syncthreads();
+            int n = 0;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) n += s_count[w];
+            over += (float)(n - K);
+        }
+    }
+    // A sum too far below its reference: again, relative to the largest term.
+    // (With candidates left over the mass below the pivot is at most V times the
+    // least of them, so only without any does it matter.)
+    float ref_below = ref, ref_over = last;
+    if (C > K ? over < 0x1p-60f : below < 0x1p-60f) {
+        const uint64_t bound = C > K ? (uint64_t)last_image << 32 : (uint64_t)order_of(from) << 32;
+        float m = -INFINITY, s = 0.f;
+        for (int v = t; v < V; v += NT) {
+            const float y = widen(z[v]);
+            m = fmaxf(m, ranked(y, 0) < bound ? y : -INFINITY);
+        }
+        __syncthreads();
+        m = block_all<NT>(m, red[0], MaxOp());
+        for (int v = t; v < V; v += NT) {
+            const float y = widen(z[v]);
+            s += ranked(y, 0) < bound && m > -INFINITY ? __builtin_amdgcn_exp2f((y - m) * c2) : 0.f;
+        }
+        s = block_all<NT>(s, red[3], AddOp());
+        ref_below = m;
+        below = s;
+        over = 0.f;
+    }
+    if (t == 0) {
+        const float a = below > 0.f ? ref_below * inv_tau + __logf(below) : -INFINITY;
+        const float b = over > 0.f ? ref_over * inv_tau + __logf(over) : -INFINITY;
+        const float m = fmaxf(a, b);
+        out.put_rest(m == -INFINITY ? m : m + __logf(__expf(a - m) + __expf(b - m)));
+    }
+}
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_top(TopArgs a, int cap, int64_t r0) {
+    const int64_t r = r0 + blockIdx.x;
+    const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0};
+    top_row<T, NT, NV>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out, cap);
+}
+
+// rows too long for the registers
+template <typename T> __global__ __launch_bounds__(1024) void k_top_long(TopArgs a, int64_t r0) {
+    __shared__ uint64_t kept[HBSJD_TOP_MAX];
+    __shared__ int hist[256], word[4];
+    __shared__ float red[16];
+    const int64_t r = r0 + blockIdx.x;
+    const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0};
+    top_by_digits<1024>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out, kept, hist, red, word);
+}
+
+template <typename T> void go(const TopArgs& a, hipStream_t s) {
+    const int vecs = a.V / kVec<T>, cap = top_cap(a.K);
+    auto held = [&](auto nt, auto nv) {
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        // enough groups for the pivot, or few enough entries to take all
+        if (vecs > NT * NV || (NT * 8 < 2 * a.K && a.V > cap)) return false;
+        by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+            hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(NT), top_lds(cap), s, a, cap, r0);
+        });
+        return true;
+    };
+    using std::integral_constant;
+#define HELD(nt, nv) held(integral_constant<int, nt>{}, integral_constant<int, nv>{})
+    if (HELD(64, 2) || HELD(64, 8) || HELD(256, 4) || HELD(512, 4) || HELD(512, 8)) return;
+#undef HELD
+    by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+        hipLaunchKernelGGL(k_top_long<T>, grid, dim3(1024), 0, s, a, r0);
+    });
 }
 
 }  // namespace
 
 void top_logits(const TopArgs& a, hipStream_t s) {
-    by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-    const dim3 block(256);
-    if (a.elem == HBSJD_ELEM_F32)
-        hipLaunchKernelGGL(k_top<float>, grid, block, 0, s, a, r0);
-    else if (a.elem == HBSJD_ELEM_BF16)
-        hipLaunchKernelGGL(k_top<Bf16>, grid, block, 0, s, a, r0);
-    else
-        hipLaunchKernelGGL(k_top<F16>, grid, block, 0, s, a, r0);
-    });
+    if (a.elem == HBSJD_ELEM_F32) go<float>(a, s);
+    else if (a.elem == HBSJD_ELEM_BF16) go<Bf16>(a, s);
+    else go<F16>(a, s);
 }
 
 }  // namespace hbsjd
