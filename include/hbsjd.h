@@ -278,6 +278,13 @@ hbsjd_status hbsjd_bikl_rows(const float* logits_s, const float* logits_t, int64
  * read nor written). Rows may start at any element. V need not be a multiple of
  * anything. All pointers are device memory of the current device.
  *
+ * Calls on long rows need a workspace of the caller's, device memory (aligned to
+ * 4 bytes) that a call uses until its kernels have run and whose contents mean
+ * nothing before or after; hbsjd_top_logits_workspace and
+ * hbsjd_distill_top_workspace say how many bytes (0 up to V = 16384 and for
+ * arguments that would be refused). EINVAL when it is smaller. Calls that may
+ * run at the same time (captured ones in graphs that may, too) need one each.
+ *
  * Data errors cannot be returned by a call that does not wait; they end up in
  * the row they belong to, as NaN, and in no other row.
  */
@@ -291,9 +298,12 @@ typedef enum hbsjd_elem {
 #define HBSJD_TOP_MAX 2048
 #define HBSJD_ADJUST_MAX_BIASES 1024
 
+uint64_t hbsjd_top_logits_workspace(int64_t rows, int32_t V, int32_t elem, int32_t K);
+uint64_t hbsjd_distill_top_workspace(int64_t rows, int32_t V, int32_t elem, int32_t K);
+
 /*
  * A teacher's answer in short form: the K largest logits of every row.
- *   values [rows][K]  fp32, in descending order, exactly the row's logits
+ *   values [rows][K]  fp32, in descending order, exactly the row's logits (-0 as +0)
  *   index  [rows][K]  their entries; the lowest index first among equal logits
  *   rest   [rows]     fp32, log of the sum over all other entries v of
  *                     exp(logits[v] / temperature); -infinity when there are
@@ -307,7 +317,8 @@ typedef enum hbsjd_elem {
  */
 hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, int32_t elem,
                                    int64_t ld, int32_t K, float temperature, float* values,
-                                   int32_t* index, float* rest, void* stream);
+                                   int32_t* index, float* rest, void* workspace,
+                                   uint64_t workspace_bytes, void* stream);
 
 /*
  * Divergence of a student's rows from a teacher's short answers, with its
@@ -357,7 +368,8 @@ typedef struct hbsjd_distill_args {
  * bits. EINVAL; EHIP.
  */
 hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* args, float* loss, void* grad,
-                                    int64_t ld_grad, void* stream);
+                                    int64_t ld_grad, void* workspace, uint64_t workspace_bytes,
+                                    void* stream);
 
 /*
  * What is done to logits ahead of a draw (hbsjd_transform_rows takes the result

@@ -82,8 +82,11 @@ _SIGS = {
     "hbsjd_score_bikl": (_I32, [_P, _P, _I32, _P, _P, _P, _P, _P]),
     "hbsjd_bikl_rows": (_I32, [_P, _P, ctypes.c_int64, _I32, _P, _P]),
     "hbsjd_top_logits_rows": (_I32, [ctypes.c_int64, _I32, _P, _I32, ctypes.c_int64, _I32,
-                                     ctypes.c_float, _P, _P, _P, _P]),
-    "hbsjd_distill_top_rows": (_I32, [ctypes.POINTER(_DistillArgs), _P, _P, ctypes.c_int64, _P]),
+                                     ctypes.c_float, _P, _P, _P, _P, ctypes.c_uint64, _P]),
+    "hbsjd_top_logits_workspace": (ctypes.c_uint64, [ctypes.c_int64, _I32, _I32, _I32]),
+    "hbsjd_distill_top_rows": (_I32, [ctypes.POINTER(_DistillArgs), _P, _P, ctypes.c_int64, _P,
+                                      ctypes.c_uint64, _P]),
+    "hbsjd_distill_top_workspace": (ctypes.c_uint64, [ctypes.c_int64, _I32, _I32, _I32]),
     "hbsjd_adjust_rows": (_I32, [ctypes.POINTER(_AdjustArgs), _P, _I32, ctypes.c_int64, _P]),
     "hbsjd_verify_probs": (_I32, [_I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "hbsjd_transform_rows": (_I32, [_I32, _I32, _P, _I32, ctypes.c_float, _P, _I32,
@@ -439,6 +442,13 @@ def _opt(t) -> _P:
     return _P(None if t is None else t.data_ptr())
 
 
+def _workspace(nbytes: int, device):
+    """Device memory for one call: allocated for the stream that the call runs on,
+    so that its next owner comes after the call's kernels."""
+    import torch
+    return (torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None), nbytes
+
+
 class _OnStream:
     """The device of `t` and a stream of it, for a call that does not wait:
     outputs are allocated for that stream, and the caching allocator keeps the
@@ -502,9 +512,11 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
         values = _vector(out[0], "values", (rows, k), torch.float32, logits.device)
         index = _vector(out[1], "index", (rows, k), torch.int32, logits.device)
         rest = _vector(out[2], "rest", (rows,), torch.float32, logits.device)
-        _check(L.hbsjd_top_logits_rows(rows, V, _opt(logits), _elem(logits.dtype), ld, k,
+        elem = _elem(logits.dtype)
+        ws, ws_bytes = _workspace(L.hbsjd_top_logits_workspace(rows, V, elem, k), logits.device)
+        _check(L.hbsjd_top_logits_rows(rows, V, _opt(logits), elem, ld, k,
                                        float(temperature), _opt(values), _opt(index), _opt(rest),
-                                       on.uses(logits, values, index, rest)),
+                                       _opt(ws), ws_bytes, on.uses(logits, values, index, rest)),
                "hbsjd_top_logits_rows")
     return values, index, rest
 
@@ -542,11 +554,13 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
             ld_grad = _matrix(grad, "grad", logits)
             if grad.dtype != logits.dtype:
                 raise ValueError("grad: expected the logits' type")
-        a = _DistillArgs(rows, V, K, _opt(logits), ld, _elem(logits.dtype), float(temperature),
+        elem = _elem(logits.dtype)
+        ws, ws_bytes = _workspace(L.hbsjd_distill_top_workspace(rows, V, elem, K), dev)
+        a = _DistillArgs(rows, V, K, _opt(logits), ld, elem, float(temperature),
                          _opt(values), _opt(index), _opt(rest), float(forward_weight),
                          float(reverse_weight), _opt(row_weight))
         _check(L.hbsjd_distill_top_rows(
-            ctypes.byref(a), _opt(loss), _opt(grad), ld_grad,
+            ctypes.byref(a), _opt(loss), _opt(grad), ld_grad, _opt(ws), ws_bytes,
             on.uses(logits, values, index, rest, row_weight, loss, grad)),
             "hbsjd_distill_top_rows")
     return loss, grad

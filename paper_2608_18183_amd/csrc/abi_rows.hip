@@ -28,6 +28,12 @@ const char* rows_problem(int64_t rows, int32_t V) {
     return nullptr;
 }
 
+const char* workspace_problem(const void* p, uint64_t bytes, uint64_t need) {
+    if (need && (!p || bytes < need)) return "workspace smaller than the call needs";
+    if (need && !aligned(p, 4)) return "workspace not aligned to 4 bytes";
+    return nullptr;
+}
+
 bool temperature_ok(float t) { return t >= 1e-6f && t <= 1e6f; }
 
 hbsjd_status launched(const char* where) {
@@ -40,9 +46,21 @@ hbsjd_status launched(const char* where) {
 
 extern "C" {
 
+uint64_t hbsjd_top_logits_workspace(int64_t rows, int32_t V, int32_t elem, int32_t K) {
+    if (rows < 1 || rows_problem(rows, V) || !elem_ok(elem) || K < 1 || K > V || K > HBSJD_TOP_MAX)
+        return 0;
+    return top_logits_workspace(rows, V, K, elem);
+}
+
+uint64_t hbsjd_distill_top_workspace(int64_t rows, int32_t V, int32_t elem, int32_t K) {
+    if (rows < 1 || rows_problem(rows, V) || !elem_ok(elem) || K < 1 || K > HBSJD_TOP_MAX) return 0;
+    return distill_top_workspace(rows, V, K, elem);
+}
+
 hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, int32_t elem,
                                    int64_t ld, int32_t K, float temperature, float* values,
-                                   int32_t* index, float* rest, void* stream) {
+                                   int32_t* index, float* rest, void* workspace,
+                                   uint64_t workspace_bytes, void* stream) {
     try {
         if (const char* why = rows_problem(rows, V)) return api_fail(HBSJD_EINVAL, why);
         if (K < 1 || K > V || K > HBSJD_TOP_MAX)
@@ -55,8 +73,11 @@ hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, 
         if (!values || !index || !rest) return api_fail(HBSJD_EINVAL, "NULL buffer");
         if (!aligned(values, 4) || !aligned(index, 4) || !aligned(rest, 4))
             return api_fail(HBSJD_EINVAL, "buffer not aligned to its elements");
+        if (const char* why = workspace_problem(workspace, workspace_bytes,
+                                                top_logits_workspace(rows, V, K, elem)))
+            return api_fail(HBSJD_EINVAL, why);
         TopArgs a{rows, V, K, logits, elem, ld, 1.f / temperature, values, index, rest};
-        top_logits(a, (hipStream_t)stream);
+        top_logits(a, workspace, (hipStream_t)stream);
         return launched("top_logits_rows");
     } catch (...) {
         return api_fail(HBSJD_EINTERNAL, "unexpected host exception in hbsjd_top_logits_rows");
@@ -64,7 +85,8 @@ hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, 
 }
 
 hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* p, float* loss, void* grad,
-                                    int64_t ld_grad, void* stream) {
+                                    int64_t ld_grad, void* workspace, uint64_t workspace_bytes,
+                                    void* stream) {
     try {
         if (!p) return api_fail(HBSJD_EINVAL, "args is NULL");
         if (const char* why = rows_problem(p->rows, p->V)) return api_fail(HBSJD_EINVAL, why);
@@ -92,9 +114,12 @@ hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* p, float* loss, vo
             if (grad == p->logits && ld_grad != p->ld)
                 return api_fail(HBSJD_EINVAL, "grad may be the logits only with their row stride");
         }
+        if (const char* why = workspace_problem(
+                workspace, workspace_bytes, distill_top_workspace(p->rows, p->V, p->K, p->elem)))
+            return api_fail(HBSJD_EINVAL, why);
         DistillArgs a{p->rows, p->V, p->K, p->logits, p->elem, p->ld, p->values, p->index, p->rest,
                       1.f / p->temperature, alpha, beta, p->row_weight, loss, grad, ld_grad};
-        distill_top(a, (hipStream_t)stream);
+        distill_top(a, workspace, (hipStream_t)stream);
         return launched("distill_top_rows");
     } catch (...) {
         return api_fail(HBSJD_EINTERNAL, "unexpected host exception in hbsjd_distill_top_rows");

@@ -15,6 +15,8 @@
 // sum, the unlisted gradient is one factor for the row times e_v.
 #include "rows.h"
 
+#include <algorithm>
+
 namespace hbsjd {
 namespace {
 
@@ -39,12 +41,14 @@ struct Entries {
 };
 inline size_t entries_bytes(int V, int K) { return ((size_t)(V + 31) / 32 + 3 * (size_t)K) * 4; }
 
-// fetches the answer, marks its entries and gathers the student's logits there
-// (before anything of the gradient is written: it may take the logits' place);
-// returns the largest t_k / tau and z_k seen by this thread
+// Fetches the answer and marks its entries that lie among the V from `first` on.
+// Their logits are gathered here (before anything of the gradient is written: it
+// may take the logits' place), or read from `gathered`. mt and mk: the largest
+// t_k / tau and z_k that this thread has seen.
 template <int NT, typename T>
 __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* z, const Span& sp,
-                                      const Entries& e, int* bad, float& mt, float& mk) {
+                                      int first, int V, const Entries& e, int* bad, float* gathered,
+                                      bool gather, float& mt, float& mk) {
     const float* tv = a.values + r * a.K;
     const int32_t* ti = a.index + r * a.K;
     for (int k = threadIdx.x; k < a.K; k += NT) {
@@ -54,12 +58,22 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
             if (v != -1) *bad = 1;
             v = -1;
         } else {
-            const int p = sp.place(v, a.V);
-            if (atomicOr(&e.listed[p >> 5], 1u << (p & 31)) >> (p & 31) & 1) *bad = 1;
-            const float y = widen(z[v]);
-            e.zk[k] = y;
-            mk = fmaxf(mk, y);
-            mt = fmaxf(mt, x);
+            const int at = v - first;
+            float y;
+            if (at >= 0 && at < V) {
+                const int p = sp.place(at, V);
+                if (atomicOr(&e.listed[p >> 5], 1u << (p & 31)) >> (p & 31) & 1) *bad = 1;
+                if (gather) {
+                    y = widen(z[at]);
+                    if (gathered) gathered[k] = y;
+                }
+            }
+            if (!gather) y = gathered[k];
+            if (!gather || !gathered) {
+                e.zk[k] = y;
+                mk = fmaxf(mk, y);
+                mt = fmaxf(mt, x);
+            }
         }
         e.entry[k] = v;
         e.tk[k] = x;
@@ -119,13 +133,13 @@ __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries&
     return w;
 }
 
-// the gradient at the listed entries
+// the gradient at the listed entries among the V from `first` on; g: of the first
 template <int NT, typename T>
 __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Entries& e,
-                                                const RowStats& w, float wt, T* g) {
+                                                const RowStats& w, float wt, T* g, int first, int V) {
     for (int k = threadIdx.x; k < a.K; k += NT) {
-        const int v = e.entry[k];
-        if (v < 0) continue;
+        const int v = e.entry[k] - first;
+        if (e.entry[k] < 0 || v < 0 || v >= V) continue;
         const float lp = e.tk[k] - w.lt, lq = (e.zk[k] - w.m) * a.inv_tau - w.lz;
         const float p = __expf(lp), q = __expf(lq);
         float d = a.alpha * (q - p);
@@ -147,94 +161,74 @@ __device__ __forceinline__ void fill_row(T* g, int V, float x) {
     if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(x);
 }
 
-// A workgroup of NT threads per row, the row in registers, NV 16-byte vectors a
-// thread: logits leave memory once. Listed entries become -infinity in the
-// registers, so that the maximum, the sum and the gradient's factor are of the
-// unlisted ones alone; their own gradient is stored over the row's afterwards.
-template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV * 4 > 32 ? 4 : 5))) void k_distill(
-    DistillArgs a, int64_t r0) {
-    constexpr int E = kVec<T>;
-    extern __shared__ uint32_t lds[];
-    __shared__ float red[8][NT / 64];
-    __shared__ int bad;
-    const int t = threadIdx.x;
-    const Entries e = Entries::in(lds, a.V, a.K);
-    const float c2 = a.inv_tau * kLog2e;
-    const int64_t r = r0 + blockIdx.x;
-    const T* z = (const T*)a.logits + r * a.ld;
-    T* g = a.grad ? (T*)a.grad + r * a.ld_grad : nullptr;
-    const float w = a.weight ? a.weight[r] : 1.f;
-    if (w == 0.f) {
-        if (g) fill_row<NT>(g, a.V, 0.f);
-        if (a.loss && t == 0) a.loss[r] = 0.f;
-        return;
-    }
-    const Span sp = Span::of(z, a.V);
+// ---- a row, or a part of one, in registers: NV 16-byte vectors a thread
+
+template <typename T, int NT, int NV> struct Held {
+    static constexpr int E = kVec<T>;
     u32x4 x[NV];
-    float xe = -INFINITY;
-    const u32x4* z4 = (const u32x4*)(z + sp.head);
-    if (sp.vecs > 0)
+    float xe;   // this thread's edge entry
+    Span sp;
+
+    __device__ __forceinline__ void load(const T* z, int V) {
+        sp = Span::of(z, V);
+        xe = -INFINITY;
+        const u32x4* z4 = (const u32x4*)(z + sp.head);
+        if (sp.vecs > 0)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min(t + NT * i, sp.vecs - 1));
-    if (t < sp.edges()) xe = widen(z[sp.edge(t, a.V)]);
-    const float rest = a.rest ? a.rest[r] : -INFINITY;
-    for (int i = t; i < (a.V + 31) / 32; i += NT) e.listed[i] = 0;
-    if (t == 0) bad = 0;
-    __syncthreads();
-    float mm[3] = {-INFINITY, -INFINITY, rest};   // maxima: unlisted, listed, teacher
-    fetch<NT>(a, r, z, sp, e, &bad, mm[2], mm[1]);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int j = t + NT * i;
-        if (j >= sp.vecs) {
-            x[i] = masked_vec<T>();
-            continue;
-        }
-        const uint32_t bits = e.listed[j * E >> 5] >> (j * E & 31);
-#pragma unroll
-        for (int q = 0; q < E; ++q) {
-            vec_mask<T>(x[i], q, bits >> q & 1);
-            mm[0] = fmaxf(mm[0], vec_get<T>(x[i], q));
-        }
-        __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min((int)threadIdx.x + NT * i, sp.vecs - 1));
+        if ((int)threadIdx.x < sp.edges()) xe = widen(z[sp.edge(threadIdx.x, V)]);
     }
-    if (t < sp.edges()) {
-        const int p = sp.vecs * E + t;
-        if (e.listed[p >> 5] >> (p & 31) & 1) xe = -INFINITY;
-    }
-    mm[0] = fmaxf(mm[0], xe);
-    block_all<NT, 3>(mm, red, MaxOp());
-    const float m0 = mm[0] == -INFINITY ? fmaxf(mm[1], mm[0]) : mm[0];
-    // fp32 rows: the exponentials take the logits' registers
-    float s = 0.f;
+    // Listed entries become -infinity, so that the maximum, the sum and the
+    // gradient's factor are of the unlisted ones alone. Returns the largest.
+    __device__ __forceinline__ float mask(const uint32_t* listed) {
+        float m = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NV; ++i) {
+            const int j = threadIdx.x + NT * i;
+            if (j >= sp.vecs) {
+                x[i] = masked_vec<T>();
+                continue;
+            }
+            const uint32_t bits = listed[j * E >> 5] >> (j * E & 31);
 #pragma unroll
-        for (int q = 0; q < E; ++q) {
-            const float y = __builtin_amdgcn_exp2f((vec_get<T>(x[i], q) - m0) * c2);
-            s += y;
-            if constexpr (E == 4) x[i][q] = __float_as_uint(y);
+            for (int q = 0; q < E; ++q) {
+                vec_mask<T>(x[i], q, bits >> q & 1);
+                m = fmaxf(m, vec_get<T>(x[i], q));
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if ((int)threadIdx.x < sp.edges()) {
+            const int p = sp.vecs * E + threadIdx.x;
+            if (listed[p >> 5] >> (p & 31) & 1) xe = -INFINITY;
+        }
+        return fmaxf(m, xe);
     }
-    const float ye = __builtin_amdgcn_exp2f((xe - m0) * c2);
-    s += ye;
-    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s, bad != 0, red + 3, red + 6);
-    if (a.loss && t == 0) a.loss[r] = w * st.loss;
-    if (g && !st.ok) fill_row<NT>(g, a.V, kNan);
-    if (g && st.ok) {
-        // (16-bit rows: the exponentials are worked out again, rather than
-        // kept in twice the registers)
+    // x becomes exp2((x - m0) c2) in fp32 rows (16-bit ones keep the logits, and
+    // work the exponentials out again when they are stored: half the registers)
+    __device__ __forceinline__ float sum(float m0, float c2) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int q = 0; q < E; ++q) {
+                const float y = __builtin_amdgcn_exp2f((vec_get<T>(x[i], q) - m0) * c2);
+                s += y;
+                if constexpr (E == 4) x[i][q] = __float_as_uint(y);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        xe = __builtin_amdgcn_exp2f((xe - m0) * c2);
+        return s + xe;
+    }
+    // f times the exponentials, after sum()
+    __device__ __forceinline__ void store(T* g, const T* z, int V, float f, float m0, float c2) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
-        const float wt = w * a.inv_tau, f = wt * st.factor;
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         T* gv = g + sp.head;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = t + NT * i;
+            const int j = threadIdx.x + NT * i;
             float y[E];
 #pragma unroll
             for (int q = 0; q < E; ++q) {
@@ -250,21 +244,23 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(NV * 4 > 32 
                 for (int q = 0; q < E; ++q) gv[j * E + q] = narrow<T>(y[q]);
             }
         }
-        if (t < sp.edges()) g[sp.edge(t, a.V)] = narrow<T>(f * ye);
-        __syncthreads();   // the row's stores are done
-        listed_gradient<NT>(a, e, st, wt, g);
+        if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(f * xe);
     }
-}
+};
 
-// Rows too long for the registers: three passes over them in memory.
-template <typename T>
-__global__ __launch_bounds__(1024) void k_distill_long(DistillArgs a, int64_t r0) {
-    constexpr int NT = 1024;
+constexpr int waves_of(int nv) { return nv > 8 ? 4 : 5; }
+
+// A workgroup of NT threads per row: logits leave memory once. The gradient at
+// the listed entries is stored over the row's afterwards.
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)))) void k_distill(
+    DistillArgs a, int64_t r0) {
     extern __shared__ uint32_t lds[];
     __shared__ float red[8][NT / 64];
     __shared__ int bad;
     const int t = threadIdx.x;
     const Entries e = Entries::in(lds, a.V, a.K);
+    const float c2 = a.inv_tau * kLog2e;
     const int64_t r = r0 + blockIdx.x;
     const T* z = (const T*)a.logits + r * a.ld;
     T* g = a.grad ? (T*)a.grad + r * a.ld_grad : nullptr;
@@ -274,34 +270,156 @@ __global__ __launch_bounds__(1024) void k_distill_long(DistillArgs a, int64_t r0
         if (a.loss && t == 0) a.loss[r] = 0.f;
         return;
     }
-    const Span sp{0, a.V, 0};
+    Held<T, NT, NV> h;
+    h.load(z, a.V);
     const float rest = a.rest ? a.rest[r] : -INFINITY;
     for (int i = t; i < (a.V + 31) / 32; i += NT) e.listed[i] = 0;
     if (t == 0) bad = 0;
     __syncthreads();
-    float mm[3] = {-INFINITY, -INFINITY, rest};
-    fetch<NT>(a, r, z, sp, e, &bad, mm[2], mm[1]);
+    float mm[3] = {-INFINITY, -INFINITY, rest};   // maxima: unlisted, listed, teacher
+    fetch<NT>(a, r, z, h.sp, 0, a.V, e, &bad, nullptr, true, mm[2], mm[1]);
     __syncthreads();
-    auto unlisted = [&](int v) { return !(e.listed[v >> 5] >> (v & 31) & 1); };
-    for (int v = t; v < a.V; v += NT)
-        if (unlisted(v)) mm[0] = fmaxf(mm[0], widen(z[v]));
+    mm[0] = h.mask(e.listed);
     block_all<NT, 3>(mm, red, MaxOp());
     const float m0 = mm[0] == -INFINITY ? fmaxf(mm[1], mm[0]) : mm[0];
-    float s = 0.f;
-    for (int v = t; v < a.V; v += NT)
-        if (unlisted(v)) s += __expf((widen(z[v]) - m0) * a.inv_tau);
-    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s, bad != 0, red + 3, red + 6);
+    const float s0 = h.sum(m0, c2);
+    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s0, bad != 0, red + 3, red + 6);
     if (a.loss && t == 0) a.loss[r] = w * st.loss;
     if (g && !st.ok) fill_row<NT>(g, a.V, kNan);
     if (g && st.ok) {
-        const float wt = w * a.inv_tau, f = wt * st.factor;
-        for (int v = t; v < a.V; v += NT)
-            if (unlisted(v)) g[v] = narrow<T>(f * __expf((widen(z[v]) - m0) * a.inv_tau));
-        listed_gradient<NT>(a, e, st, wt, g);
+        const float wt = w * a.inv_tau;
+        h.store(g, z, a.V, wt * st.factor, m0, c2);
+        __syncthreads();   // the row's stores come first
+        listed_gradient<NT>(a, e, st, wt, g, 0, a.V);
     }
 }
 
-template <typename T> void go(const DistillArgs& a, hipStream_t s) {
+// Rows too long for a workgroup's registers, or long and few: `parts` workgroups
+// a row, in two launches. The first leaves each part's unlisted maximum and sum,
+// and the listed entries' logits, in the workspace; the second joins them (every
+// part's workgroup works the classes out for itself) and writes the gradient. The
+// part is read again then, mostly from the caches: rows are taken in slabs that
+// fit them.
+struct PartsArgs {
+    int parts, len;
+    float* zk;       // [rows of the slab][K]
+    float* stats;    // [rows of the slab][parts][3]: maximum, sum, whether refused
+};
+
+template <typename T, int NT, int NV, bool Second>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)))) void k_distill_part(
+    DistillArgs a, PartsArgs p, int64_t r0) {
+    extern __shared__ uint32_t lds[];
+    __shared__ float red[8][NT / 64];
+    __shared__ int bad;
+    const int t = threadIdx.x;
+    const Entries e = Entries::in(lds, p.len, a.K);
+    const float c2 = a.inv_tau * kLog2e;
+    const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
+    const int64_t r = r0 + row;
+    const int first = c * p.len, V = min(p.len, a.V - first);
+    const T* z = (const T*)a.logits + r * a.ld + first;
+    T* g = a.grad ? (T*)a.grad + r * a.ld_grad + first : nullptr;
+    const float w = a.weight ? a.weight[r] : 1.f;
+    if (w == 0.f) {
+        if (Second && g) fill_row<NT>(g, V, 0.f);
+        if (Second && a.loss && c == 0 && t == 0) a.loss[r] = 0.f;
+        return;
+    }
+    Held<T, NT, NV> h;
+    // the loss alone takes one workgroup a row, which needs no logits
+    if (!Second || g) h.load(z, V);
+    else if (c > 0) return;
+    else h.sp = Span::of(z, V);
+    const float rest = a.rest ? a.rest[r] : -INFINITY;
+    float* zk = p.zk + (int64_t)row * a.K;
+    float* stats = p.stats + (int64_t)row * p.parts * 3;
+    for (int i = t; i < (V + 31) / 32; i += NT) e.listed[i] = 0;
+    if (t == 0) bad = 0;
+    __syncthreads();
+    float mm[3] = {-INFINITY, -INFINITY, rest};
+    fetch<NT>(a, r, z, h.sp, first, V, e, &bad, zk, !Second, mm[2], mm[1]);
+    __syncthreads();
+    if constexpr (!Second) {
+        float m0 = block_all<NT>(h.mask(e.listed), red[0], MaxOp());
+        // relative to a finite number: a part without an unlisted mass sums to 0
+        const float s = block_all<NT>(h.sum(m0 == -INFINITY ? 0.f : m0, c2), red[1], AddOp());
+        if (t == 0) {
+            stats[3 * c] = m0;
+            stats[3 * c + 1] = s;
+            stats[3 * c + 2] = bad;
+        }
+    } else {
+        bool refused = bad != 0;
+        float m0 = -INFINITY, s0 = 0.f;
+        for (int i = 0; i < p.parts; ++i) {
+            m0 = fmaxf(m0, stats[3 * i]);
+            refused |= stats[3 * i + 2] != 0.f;
+        }
+        block_all<NT, 2>(*(float(*)[2])(mm + 1), red, MaxOp());
+        if (m0 == -INFINITY) m0 = mm[1];
+        for (int i = 0; i < p.parts; ++i) {
+            const float m = stats[3 * i], s = stats[3 * i + 1];
+            s0 += m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - m0) * c2);
+        }
+        const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], t == 0 ? s0 : 0.f, refused, red + 3,
+                                        red + 6);
+        if (a.loss && c == 0 && t == 0) a.loss[r] = w * st.loss;
+        if (!g) return;
+        if (!st.ok) {
+            fill_row<NT>(g, V, kNan);
+            return;
+        }
+        const float wt = w * a.inv_tau;
+        h.mask(e.listed);
+        h.sum(m0, c2);
+        h.store(g, z, V, wt * st.factor, m0, c2);
+        __syncthreads();
+        listed_gradient<NT>(a, e, st, wt, g, first, V);
+    }
+}
+
+// How a call runs: whole rows, or in parts with workspace for `slab` rows.
+struct Plan {
+    int parts = 0, len = 0;
+    int64_t slab = 0;
+};
+constexpr int kPart = 16384;   // entries of a part at most
+
+inline size_t part_row_bytes(const Plan& p, int K) { return ((size_t)K + 3 * (size_t)p.parts) * 4; }
+
+// Parts where a workgroup cannot hold the row, and for long rows that are fewer
+// than the CUs: then enough of them for two workgroups a CU, of 4096 entries at
+// least.
+Plan plan_of(int64_t rows, int V, int K, int32_t elem) {
+    Plan p;
+    const int64_t size = elem_size(elem);
+    const int64_t held = 1024 * (elem == HBSJD_ELEM_F32 ? 8 : 16) * (16 / size);
+    if (V <= kPart || (V <= held && rows >= 256)) return p;
+    p.parts = (V + kPart - 1) / kPart;
+    while (rows * p.parts < 512 && V / (2 * p.parts) >= 4096) p.parts *= 2;
+    p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
+    p.parts = (V + p.len - 1) / p.len;
+    // a slab's logits and gradient together stay within the last-level cache
+    p.slab = std::max<int64_t>(1, (96 << 20) / (V * size));
+    p.slab = std::min(p.slab, rows);
+    return p;
+}
+
+template <typename T> void go_parts(const DistillArgs& a, const Plan& plan, void* ws, hipStream_t s) {
+    constexpr int NT = 512, NV = kPart / kVec<T> / NT;
+    PartsArgs p{plan.parts, plan.len, (float*)ws, (float*)ws + plan.slab * a.K};
+    const size_t lds = entries_bytes(p.len, a.K);
+    for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
+        const dim3 grid((unsigned)(std::min(plan.slab, a.rows - r0) * p.parts));
+        hipLaunchKernelGGL((k_distill_part<T, NT, NV, false>), grid, dim3(NT), lds, s, a, p, r0);
+        hipLaunchKernelGGL((k_distill_part<T, NT, NV, true>), grid, dim3(NT), lds, s, a, p, r0);
+    }
+}
+
+template <typename T> void go(const DistillArgs& a, void* ws, hipStream_t s) {
+    const Plan plan = plan_of(a.rows, a.V, a.K, a.elem);
+    if (plan.parts) return go_parts<T>(a, plan, ws, s);
     const size_t lds = entries_bytes(a.V, a.K);
     const int vecs = a.V / kVec<T>;
     auto held = [&](auto nt, auto nv) {
@@ -311,27 +429,28 @@ template <typename T> void go(const DistillArgs& a, hipStream_t s) {
         });
     };
     using std::integral_constant;
-#define HOLD(nt, nv) held(integral_constant<int, nt>{}, integral_constant<int, nv>{})
-    if (vecs <= 64 * 2) HOLD(64, 2);
-    else if (vecs <= 64 * 8) HOLD(64, 8);
-    else if (vecs <= 256 * 4) HOLD(256, 4);
-    else if (vecs <= 256 * 8) HOLD(256, 8);
-    else if (vecs <= 512 * 8) HOLD(512, 8);
-    else if (vecs <= 1024 * 8) HOLD(1024, 8);
-    else if (vecs <= 1024 * 16) HOLD(1024, 16);
-    else
-        by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-            hipLaunchKernelGGL(k_distill_long<T>, grid, dim3(1024), lds, s, a, r0);
-        });
-#undef HOLD
+#define HELD(nt, nv) held(integral_constant<int, nt>{}, integral_constant<int, nv>{})
+    if (vecs <= 64 * 2) HELD(64, 2);
+    else if (vecs <= 64 * 8) HELD(64, 8);
+    else if (vecs <= 256 * 4) HELD(256, 4);
+    else if (vecs <= 256 * 8) HELD(256, 8);
+    else if (vecs <= 512 * 8) HELD(512, 8);
+    else if (vecs <= 1024 * 8) HELD(1024, 8);
+    else if constexpr (sizeof(T) == 2) HELD(1024, 16);
+#undef HELD
 }
 
 }  // namespace
 
-void distill_top(const DistillArgs& a, hipStream_t s) {
-    if (a.elem == HBSJD_ELEM_F32) go<float>(a, s);
-    else if (a.elem == HBSJD_ELEM_BF16) go<Bf16>(a, s);
-    else go<F16>(a, s);
+size_t distill_top_workspace(int64_t rows, int V, int K, int32_t elem) {
+    const Plan p = plan_of(rows, V, K, elem);
+    return p.parts ? p.slab * part_row_bytes(p, K) : 0;
+}
+
+void distill_top(const DistillArgs& a, void* workspace, hipStream_t s) {
+    if (a.elem == HBSJD_ELEM_F32) go<float>(a, workspace, s);
+    else if (a.elem == HBSJD_ELEM_BF16) go<Bf16>(a, workspace, s);
+    else go<F16>(a, workspace, s);
 }
 
 }  // namespace hbsjd

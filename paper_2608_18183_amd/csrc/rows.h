@@ -191,7 +191,9 @@ struct TopArgs {
     int32_t* index;   // [rows][K]
     float* rest;      // [rows]
 };
-void top_logits(const TopArgs& a, hipStream_t s);
+// bytes of workspace that a call needs
+size_t top_logits_workspace(int64_t rows, int V, int K, int32_t elem);
+void top_logits(const TopArgs& a, void* workspace, hipStream_t s);
 
 struct DistillArgs {
     int64_t rows;
@@ -208,7 +210,9 @@ struct DistillArgs {
     void* grad;             // [rows], stride ld_grad, or null
     int64_t ld_grad;
 };
-void distill_top(const DistillArgs& a, hipStream_t s);
+// bytes of workspace that a call needs
+size_t distill_top_workspace(int64_t rows, int V, int K, int32_t elem);
+void distill_top(const DistillArgs& a, void* workspace, hipStream_t s);
 
 struct AdjustArgs {
     int64_t rows;

@@ -20,6 +20,8 @@
 // and a bitonic sort instead, with the same results.
 #include "rows.h"
 
+#include <algorithm>
+
 namespace hbsjd {
 namespace {
 
@@ -460,42 +462,116 @@ __global__ __launch_bounds__(NT) void k_top(TopArgs a, int cap, int64_t r0) {
     top_row<T, NT, NV>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out, cap);
 }
 
-// rows too long for the registers
-template <typename T> __global__ __launch_bounds__(1024) void k_top_long(TopArgs a, int64_t r0) {
-    __shared__ uint64_t kept[HBSJD_TOP_MAX];
-    __shared__ int hist[256], word[4];
-    __shared__ float red[16];
-    const int64_t r = r0 + blockIdx.x;
-    const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0};
-    top_by_digits<1024>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out, kept, hist, red, word);
+// Long rows: every part's K largest and the mass of its others go to the
+// workspace, and the row's are the K largest of the parts'. Lists are in
+// descending order with the lowest index first and parts follow one another, so
+// equal logits keep the order of their entries.
+struct PartsArgs {
+    int parts, len;
+    float* values;   // [rows of the slab][parts][K]
+    int32_t* index;
+    float* rest;     // [rows of the slab][parts]
+};
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_top_part(TopArgs a, PartsArgs p, int cap, int64_t r0) {
+    const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
+    const int first = c * p.len;
+    const int64_t at = blockIdx.x;
+    const TopRow out{p.values + at * a.K, p.index + at * a.K, p.rest + at, nullptr, nullptr, 0, first};
+    top_row<T, NT, NV>((const T*)a.logits + (r0 + row) * a.ld + first, min(p.len, a.V - first), a.K,
+                       a.inv_tau, out, cap);
 }
 
-template <typename T> void go(const TopArgs& a, hipStream_t s) {
-    const int vecs = a.V / kVec<T>, cap = top_cap(a.K);
-    auto held = [&](auto nt, auto nv) {
-        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-        // enough groups for the pivot, or few enough entries to take all
-        if (vecs > NT * NV || (NT * 8 < 2 * a.K && a.V > cap)) return false;
-        by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-            hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(NT), top_lds(cap), s, a, cap, r0);
+template <int NT, int NV>
+__global__ __launch_bounds__(NT) void k_top_join(TopArgs a, PartsArgs p, int cap, int64_t r0) {
+    const int64_t row = blockIdx.x, r = r0 + row, n = (int64_t)p.parts * a.K;
+    const TopRow out{a.values + r * a.K,  a.index + r * a.K, a.rest + r, p.index + row * n,
+                     p.rest + row * p.parts, p.parts,           0};
+    top_row<float, NT, NV>(p.values + row * n, (int)n, a.K, a.inv_tau, out, cap);
+}
+
+// How a call runs: whole rows, or in parts with workspace for `slab` rows.
+struct Plan {
+    int parts = 0, len = 0;
+    int64_t slab = 0;
+};
+constexpr int kPart = 16384;   // entries of a part at most
+
+inline size_t part_row_bytes(const Plan& p, int K) { return (size_t)p.parts * (8 * (size_t)K + 4); }
+
+// Rows of more entries than a workgroup holds go in parts; where rows are few,
+// in more and smaller ones, as long as the join stays the smaller work.
+Plan plan_of(int64_t rows, int V, int K) {
+    Plan p;
+    if (V <= kPart) return p;
+    p.parts = (V + kPart - 1) / kPart;
+    while (rows * p.parts < 512 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
+        p.parts *= 2;
+    p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
+    p.parts = (V + p.len - 1) / p.len;
+    p.slab = std::max<int64_t>(1, (64 << 20) / (int64_t)part_row_bytes(p, K));
+    p.slab = std::min(p.slab, rows);
+    return p;
+}
+
+// f(threads, vectors a thread) for the smallest workgroup that holds `vecs`
+// vectors and has groups enough for the pivot, or so few entries that all may be
+// candidates
+template <int NT, int NV, typename F> bool try_size(int vecs, int V, int K, F f) {
+    if (vecs > NT * NV || (NT * 8 < 2 * K && V > top_cap(K))) return false;
+    f(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{});
+    return true;
+}
+template <typename T, typename F> void by_size(int V, int K, F f) {
+    const int vecs = V / kVec<T>;
+    if (try_size<64, 2>(vecs, V, K, f) || try_size<64, 8>(vecs, V, K, f) ||
+        try_size<256, 4>(vecs, V, K, f) || try_size<512, 4>(vecs, V, K, f))
+        return;
+    if constexpr (sizeof(T) == 4) try_size<512, 8>(vecs, V, K, f) || try_size<1024, 8>(vecs, V, K, f);
+}
+
+template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
+    const int cap = top_cap(a.K);
+    const Plan plan = plan_of(a.rows, a.V, a.K);
+    if (!plan.parts) {
+        by_size<T>(a.V, a.K, [&](auto nt, auto nv) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+            by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+                hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(NT), top_lds(cap), s, a, cap, r0);
+            });
         });
-        return true;
-    };
-    using std::integral_constant;
-#define HELD(nt, nv) held(integral_constant<int, nt>{}, integral_constant<int, nv>{})
-    if (HELD(64, 2) || HELD(64, 8) || HELD(256, 4) || HELD(512, 4) || HELD(512, 8)) return;
-#undef HELD
-    by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-        hipLaunchKernelGGL(k_top_long<T>, grid, dim3(1024), 0, s, a, r0);
-    });
+        return;
+    }
+    PartsArgs p{plan.parts, plan.len, (float*)ws, nullptr, nullptr};
+    p.index = (int32_t*)(p.values + plan.slab * plan.parts * a.K);
+    p.rest = (float*)(p.index + plan.slab * plan.parts * a.K);
+    for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
+        const int64_t n = std::min(plan.slab, a.rows - r0);
+        by_size<T>(p.len, a.K, [&](auto nt, auto nv) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+            hipLaunchKernelGGL((k_top_part<T, NT, NV>), dim3((unsigned)(n * p.parts)), dim3(NT),
+                               top_lds(cap), s, a, p, cap, r0);
+        });
+        by_size<float>(p.parts * a.K, a.K, [&](auto nt, auto nv) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+            hipLaunchKernelGGL((k_top_join<NT, NV>), dim3((unsigned)n), dim3(NT), top_lds(cap), s, a, p,
+                               cap, r0);
+        });
+    }
 }
 
 }  // namespace
 
-void top_logits(const TopArgs& a, hipStream_t s) {
-    if (a.elem == HBSJD_ELEM_F32) go<float>(a, s);
-    else if (a.elem == HBSJD_ELEM_BF16) go<Bf16>(a, s);
-    else go<F16>(a, s);
+size_t top_logits_workspace(int64_t rows, int V, int K, int32_t) {
+    const Plan p = plan_of(rows, V, K);
+    return p.parts ? p.slab * part_row_bytes(p, K) : 0;
+}
+
+void top_logits(const TopArgs& a, void* workspace, hipStream_t s) {
+    if (a.elem == HBSJD_ELEM_F32) go<float>(a, workspace, s);
+    else if (a.elem == HBSJD_ELEM_BF16) go<Bf16>(a, workspace, s);
+    else go<F16>(a, workspace, s);
 }
 
 }  // namespace hbsjd

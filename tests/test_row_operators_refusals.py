@@ -25,7 +25,7 @@ def _status(st):
 
 def _top(**kw):
     a = dict(rows=2, V=100, logits=A, elem=0, ld=100, K=5, temperature=1.0, values=A, index=A,
-             rest=A, stream=None)
+             rest=A, workspace=None, workspace_bytes=0, stream=None)
     assert set(kw) <= set(a)
     a.update(kw)
     return _status(P.load_library().hbsjd_top_logits_rows(*a.values()))
@@ -49,13 +49,14 @@ def test_no_rows_is_no_work():
     assert _adjust(rows=0) == "OK"
 
 
-def _distill(loss=A, grad=A, ld_grad=100, **kw):
+def _distill(loss=A, grad=A, ld_grad=100, workspace=None, workspace_bytes=0, **kw):
     a = dict(rows=2, V=100, K=5, logits=2 * A, ld=100, elem=0, temperature=1.0, values=A, index=A,
              rest=A, forward_weight=0.5, reverse_weight=0.5, row_weight=None)
     assert set(kw) <= set(a)
     a.update(kw)
     s = B._DistillArgs(*a.values())
-    return _status(P.load_library().hbsjd_distill_top_rows(ctypes.byref(s), loss, grad, ld_grad, None))
+    return _status(P.load_library().hbsjd_distill_top_rows(ctypes.byref(s), loss, grad, ld_grad,
+                                                           workspace, workspace_bytes, None))
 
 
 @pytest.mark.parametrize("bad", [
@@ -69,8 +70,26 @@ def test_distill_refuses(bad):
     assert _distill(**bad) == "EINVAL"
 
 
+def test_long_rows_need_their_workspace():
+    L = P.load_library()
+    for f, call in ((L.hbsjd_top_logits_workspace, _top), (L.hbsjd_distill_top_workspace, _distill)):
+        for V in (1, 100, 16384):
+            assert f(5, V, 0, min(V, 5)) == 0
+        need = f(2, 200000, 0, 5)
+        assert need > 0
+        long = dict(V=200000, ld=200000, **({"ld_grad": 200000} if call is _distill else {}))
+        assert call(**long) == "EINVAL"
+        assert call(workspace=A, workspace_bytes=need - 1, **long) == "EINVAL"
+        assert call(workspace=A + 2, workspace_bytes=need, **long) == "EINVAL"
+        for bad in ((0, 200000, 0, 5), (5, 300000, 0, 5), (5, 200000, 4, 5), (5, 200000, 0, 0),
+                    (5, 200000, 0, 4000)):
+            assert f(*bad) == 0
+        # bounded, however many rows
+        assert f((1 << 31) - 1, 262144, 0, 2048) <= 256 << 20
+
+
 def test_distill_refuses_null_args():
-    assert _status(P.load_library().hbsjd_distill_top_rows(None, A, A, 100, None)) == "EINVAL"
+    assert _status(P.load_library().hbsjd_distill_top_rows(None, A, A, 100, None, 0, None)) == "EINVAL"
     assert _status(P.load_library().hbsjd_adjust_rows(None, A, 0, 100, None)) == "EINVAL"
 
 
