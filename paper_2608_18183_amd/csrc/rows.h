@@ -169,14 +169,15 @@ template <int NT, typename F> __device__ __forceinline__ float block_all(float v
     return a[0];
 }
 
-// Launches of a workgroup per item, in slabs: one launch of them all could pass
-// the 2^32 work items that a launch may have. (Workgroups that loop over items
-// hold whatever the compiler moves out of the loop: 96 registers and spills in
-// place of 81 in the divergence of fp32 rows of 16384.)
-template <typename F> inline void by_slabs(int64_t items, F f) {
-    constexpr int64_t kSlab = 1 << 21;
-    for (int64_t i0 = 0; i0 < items; i0 += kSlab)
-        f(i0, dim3((unsigned)(items - i0 < kSlab ? items - i0 : kSlab)));
+// Launches over slabs of rows: one launch of all rows could pass the 2^32 work
+// items that a launch may have. (Workgroups that loop over rows hold whatever
+// the compiler moves out of the loop: 96 registers and spills in place of 81 in
+// the divergence of fp32 rows of 16384.) f(first row, grid) with `parts`
+// workgroups a row.
+template <typename F> inline void by_slabs(int64_t rows, F f, int parts = 1) {
+    const int64_t slab = (1 << 21) / parts;
+    for (int64_t r0 = 0; r0 < rows; r0 += slab)
+        f(r0, dim3((unsigned)((rows - r0 < slab ? rows - r0 : slab) * parts)));
 }
 
 // ------------------------------------------------------------ launchers
