@@ -24,6 +24,7 @@ VERIFY_PROB, VERIFY_GREEDY, VERIFY_AR, VERIFY_AR_GREEDY = 0, 1, 2, 3
 PROGRESS_INDEPENDENT, PROGRESS_SYNC = 0, 1
 KERNELS = ["setup", "embed", "qkv", "attn", "oproj", "norm", "w13", "w2", "lmhead",
            "transform", "verify", "bikl"]
+_WHOLE_ROWS = 16384   # rows of more entries may need a workspace
 _STATUS = {0: "OK", 1: "EINVAL", 2: "ENOMEM", 3: "EHIP", 4: "ESTATE", 5: "EINTERNAL"}
 
 _P = ctypes.c_void_p
@@ -388,108 +389,93 @@ def hbsjd_bikl_rows(logits_s, logits_t, stream=None):
     return out
 
 
+# The calls below take 5 us on the GPU where rows are few, so that the time of a
+# call is the host's: checks that pass cost one comparison each, pointers go to
+# ctypes as plain integers.
+
 def _elem(dtype) -> int:
     import torch
-    try:
-        return {torch.float32: ELEM_F32, torch.bfloat16: ELEM_BF16,
-                torch.float16: ELEM_F16}[dtype]
-    except KeyError:
-        raise ValueError(f"rows of logits are fp32, bf16 or fp16, not {dtype}") from None
+    if dtype is torch.float32:
+        return ELEM_F32
+    if dtype is torch.bfloat16:
+        return ELEM_BF16
+    if dtype is torch.float16:
+        return ELEM_F16
+    raise ValueError(f"rows of logits are fp32, bf16 or fp16, not {dtype}")
 
 
 def _matrix(t, what: str, like=None):
-    """A device tensor [rows, V] whose rows are contiguous: its row stride."""
+    """A device tensor [rows, V] whose rows are contiguous: (rows, V, row stride)."""
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what}: expected a device tensor [rows, V]")
+    rows, V = t.shape
     if like is not None and (t.shape != like.shape or t.device != like.device):
         raise ValueError(f"{what}: expected shape {tuple(like.shape)} on {like.device}")
-    rows, V = t.shape
-    if V > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if V > 1 and step != 1:
         raise ValueError(f"{what}: the entries of a row have to be adjacent")
-    if rows > 1 and t.stride(0) < V:
+    if rows <= 1:
+        ld = V
+    elif ld < V:
         raise ValueError(f"{what}: rows overlap")
-    return t.stride(0) if rows > 1 else V
+    return rows, V, ld
 
 
 def _vector(t, what: str, shape, dtype, device):
-    """A contiguous device tensor of this shape and type, or None."""
-    import torch
+    """The address of a contiguous device tensor of this shape and type, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}")
     if t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor on {device}")
-    return t
+    return t.data_ptr()
 
 
 def _lists(t, what: str, rows: int, dtype, device):
     """Lists of one length for every row, [rows, n], or [n] for all rows: their
     length and row stride."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+    if t.dtype is not dtype or t.device != device:
         raise ValueError(f"{what}: expected {dtype} on {device}")
-    if t.dim() not in (1, 2) or (t.dim() == 2 and t.shape[0] != rows):
+    shape = t.shape
+    if len(shape) not in (1, 2) or (len(shape) == 2 and shape[0] != rows):
         raise ValueError(f"{what}: expected shape [{rows}, n] or [n]")
-    n = t.shape[-1]
+    n = shape[-1]
     if n > 1 and t.stride(-1) != 1:
         raise ValueError(f"{what}: the entries of a list have to be adjacent")
-    return n, t.stride(0) if t.dim() == 2 and rows > 1 else 0
-
-
-def _opt(t) -> _P:
-    return _P(None if t is None else t.data_ptr())
+    return n, t.stride(0) if len(shape) == 2 and rows > 1 else 0
 
 
 def _workspace(nbytes: int, device):
     """Device memory for one call: allocated for the stream that the call runs on,
     so that its next owner comes after the call's kernels."""
     import torch
-    return (torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None), nbytes
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
-class _OnStream:
-    """The device of `t` and a stream of it, for a call that does not wait:
-    outputs are allocated for that stream, and the caching allocator keeps the
-    inputs until it has run."""
-
-    def __init__(self, t, stream):
-        import torch
-        self._device = torch.cuda.device(t.device)
-        self._stream = None
-        if stream is not None and not hasattr(stream, "cuda_stream"):
-            stream = (torch.cuda.ExternalStream(int(stream), device=t.device) if int(stream)
-                      else torch.cuda.default_stream(t.device))
-        if stream is not None:
-            if stream.device != t.device:
-                raise ValueError(f"the stream is on {stream.device}, the logits on {t.device}")
-            if stream != torch.cuda.current_stream(t.device):
-                self._stream = stream
-        self._handle = None if stream is None else stream.cuda_stream
-
-    def __enter__(self):
-        import torch
-        self._device.__enter__()
-        if self._stream is not None:
-            self._context = torch.cuda.stream(self._stream)
-            self._context.__enter__()
-        if self._handle is None:
-            self._handle = torch.cuda.current_stream().cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        if self._stream is not None:
-            self._context.__exit__(*exc)
-        self._device.__exit__(*exc)
-
-    def uses(self, *tensors) -> _P:
-        """The stream's handle, after noting that it uses these tensors."""
-        if self._stream is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self._stream)
-        return _P(self._handle)
+def _on_stream(call, device, stream, tensors):
+    """call(handle) with the current device and stream being `device` and `stream`
+    (None: the device's current one), so that outputs are allocated for that
+    stream. The caching allocator is told that the stream uses `tensors`: the
+    calls do not wait, and the caller may drop them at once."""
+    import torch
+    if stream is None:
+        if device.index == torch.cuda.current_device():
+            return call(torch._C._cuda_getCurrentRawStream(device.index))
+        with torch.cuda.device(device):
+            return call(torch.cuda.current_stream().cuda_stream)
+    if not hasattr(stream, "cuda_stream"):
+        stream = (torch.cuda.ExternalStream(int(stream), device=device) if int(stream)
+                  else torch.cuda.default_stream(device))
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the logits on {device}")
+    with torch.cuda.stream(stream):
+        out = call(stream.cuda_stream)
+        for t in tensors:
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        return out
 
 
 def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None, out=None):
@@ -498,27 +484,30 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
     fp32 [rows]), written into `out` when given. Asynchronous on `stream` (the
     current one by default), as are the two calls below."""
     import torch
-    ld = _matrix(logits, "logits")
-    rows, V = logits.shape
-    k = int(k)
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev, k = _elem(logits.dtype), logits.device, int(k)
     if k < 1:
         raise ValueError("need k >= 1")
     L = load_library()
-    with _OnStream(logits, stream) as on:
+
+    def call(handle):
         if out is None:
-            out = (torch.empty((rows, k), dtype=torch.float32, device=logits.device),
-                   torch.empty((rows, k), dtype=torch.int32, device=logits.device),
-                   torch.empty(rows, dtype=torch.float32, device=logits.device))
-        values = _vector(out[0], "values", (rows, k), torch.float32, logits.device)
-        index = _vector(out[1], "index", (rows, k), torch.int32, logits.device)
-        rest = _vector(out[2], "rest", (rows,), torch.float32, logits.device)
-        elem = _elem(logits.dtype)
-        ws, ws_bytes = _workspace(L.hbsjd_top_logits_workspace(rows, V, elem, k), logits.device)
-        _check(L.hbsjd_top_logits_rows(rows, V, _opt(logits), elem, ld, k,
-                                       float(temperature), _opt(values), _opt(index), _opt(rest),
-                                       _opt(ws), ws_bytes, on.uses(logits, values, index, rest)),
-               "hbsjd_top_logits_rows")
-    return values, index, rest
+            values = logits.new_empty((rows, k), dtype=torch.float32)
+            index = logits.new_empty((rows, k), dtype=torch.int32)
+            rest = logits.new_empty((rows,), dtype=torch.float32)
+        else:
+            values, index, rest = out
+        nbytes = L.hbsjd_top_logits_workspace(rows, V, elem, k) if V > _WHOLE_ROWS else 0
+        ws = _workspace(nbytes, dev)
+        _check(L.hbsjd_top_logits_rows(
+            rows, V, logits.data_ptr(), elem, ld, k, temperature,
+            _vector(values, "values", (rows, k), torch.float32, dev),
+            _vector(index, "index", (rows, k), torch.int32, dev),
+            _vector(rest, "rest", (rows,), torch.float32, dev),
+            None if ws is None else ws.data_ptr(), nbytes, handle), "hbsjd_top_logits_rows")
+        return values, index, rest
+
+    return _on_stream(call, dev, stream, (logits, *(out or ())))
 
 
 def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float = 1.0,
@@ -530,40 +519,40 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
     [rows]. Returns (loss fp32 [rows], grad like logits). grad=False leaves the
     gradient out (None), a tensor is written (the logits themselves too)."""
     import torch
-    ld = _matrix(logits, "logits")
-    rows, V = logits.shape
-    dev = logits.device
-    if not isinstance(values, torch.Tensor) or values.dim() != 2:
-        raise ValueError(f"values: expected shape [{rows}, K]")
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev = _elem(logits.dtype), logits.device
+    if values is None or index is None or values.dim() != 2:
+        raise ValueError(f"values and index: expected tensors of shape [{rows}, K]")
     K = values.shape[1]
-    _vector(values, "values", (rows, K), torch.float32, dev)
-    if index is None:
-        raise ValueError("index: expected a tensor")
-    _vector(index, "index", (rows, K), torch.int32, dev)
-    _vector(rest, "rest", (rows,), torch.float32, dev)
-    _vector(row_weight, "row_weight", (rows,), torch.float32, dev)
+    f32 = torch.float32
+    a = _DistillArgs(rows, V, K, logits.data_ptr(), ld, elem, temperature,
+                     _vector(values, "values", (rows, K), f32, dev),
+                     _vector(index, "index", (rows, K), torch.int32, dev),
+                     _vector(rest, "rest", (rows,), f32, dev), forward_weight, reverse_weight,
+                     _vector(row_weight, "row_weight", (rows,), f32, dev))
     L = load_library()
-    with _OnStream(logits, stream) as on:
-        loss = torch.empty(rows, dtype=torch.float32, device=dev)
-        if grad is True:
-            grad = torch.empty((rows, V), dtype=logits.dtype, device=dev)
-        elif grad is False:
-            grad = None
-        ld_grad = 0
-        if grad is not None:
-            ld_grad = _matrix(grad, "grad", logits)
-            if grad.dtype != logits.dtype:
+
+    def call(handle):
+        loss = logits.new_empty((rows,), dtype=f32)
+        g = grad
+        if g is True:
+            g = logits.new_empty((rows, V))
+        ld_grad, address = 0, None
+        if g is False:
+            g = None
+        if g is not None:
+            ld_grad = _matrix(g, "grad", logits)[2]
+            if g.dtype is not logits.dtype:
                 raise ValueError("grad: expected the logits' type")
-        elem = _elem(logits.dtype)
-        ws, ws_bytes = _workspace(L.hbsjd_distill_top_workspace(rows, V, elem, K), dev)
-        a = _DistillArgs(rows, V, K, _opt(logits), ld, elem, float(temperature),
-                         _opt(values), _opt(index), _opt(rest), float(forward_weight),
-                         float(reverse_weight), _opt(row_weight))
-        _check(L.hbsjd_distill_top_rows(
-            ctypes.byref(a), _opt(loss), _opt(grad), ld_grad, _opt(ws), ws_bytes,
-            on.uses(logits, values, index, rest, row_weight, loss, grad)),
-            "hbsjd_distill_top_rows")
-    return loss, grad
+            address = g.data_ptr()
+        nbytes = L.hbsjd_distill_top_workspace(rows, V, elem, K) if V > _WHOLE_ROWS else 0
+        ws = _workspace(nbytes, dev)
+        _check(L.hbsjd_distill_top_rows(ctypes.byref(a), loss.data_ptr(), address, ld_grad,
+                                        None if ws is None else ws.data_ptr(), nbytes, handle),
+               "hbsjd_distill_top_rows")
+        return loss, g
+
+    return _on_stream(call, dev, stream, (logits, values, index, rest, row_weight, grad))
 
 
 def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, presence=None,
@@ -577,47 +566,53 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     new tensor of out_dtype (the logits' type by default; fp32 is what
     hbsjd_transform_rows takes), or `out`, which may be the logits."""
     import torch
-    ld = _matrix(logits, "logits")
-    rows, V = logits.shape
-    dev = logits.device
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev = _elem(logits.dtype), logits.device
+    i32, f32, row = torch.int32, torch.float32, (rows,)
     n_tokens = ld_tokens = n_bias = ld_bias = n_masks = 0
+    at = dict.fromkeys(("tokens", "bias_index", "bias_value", "mask"))
     if tokens is not None:
-        n_tokens, ld_tokens = _lists(tokens, "tokens", rows, torch.int32, dev)
-    elif any(t is not None for t in (token_count, repetition, presence, frequency)):
+        n_tokens, ld_tokens = _lists(tokens, "tokens", rows, i32, dev)
+        at["tokens"] = tokens.data_ptr()
+    elif not (token_count is repetition is presence is frequency is None):
         raise ValueError("penalties without tokens")
     if (bias_index is None) != (bias_value is None):
         raise ValueError("bias_index and bias_value go together")
     if bias_index is not None:
-        n_bias, ld_bias = _lists(bias_index, "bias_index", rows, torch.int32, dev)
-        if _lists(bias_value, "bias_value", rows, torch.float32, dev) != (n_bias, ld_bias):
+        n_bias, ld_bias = _lists(bias_index, "bias_index", rows, i32, dev)
+        if _lists(bias_value, "bias_value", rows, f32, dev) != (n_bias, ld_bias):
             raise ValueError("bias_index and bias_value have to be laid out alike")
+        at["bias_index"], at["bias_value"] = bias_index.data_ptr(), bias_value.data_ptr()
     if mask is not None:
         n_masks = mask.shape[0]
-        _vector(mask, "mask", (n_masks, (V + 31) // 32), torch.int32, dev)
+        at["mask"] = _vector(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
         if n_masks == 0:
             raise ValueError("mask: no masks")
-    for t, what, dtype in ((token_count, "token_count", torch.int32),
-                           (repetition, "repetition", torch.float32),
-                           (presence, "presence", torch.float32),
-                           (frequency, "frequency", torch.float32),
-                           (mask_row, "mask_row", torch.int32)):
-        _vector(t, what, (rows,), dtype, dev)
+    a = _AdjustArgs(rows, V, elem, logits.data_ptr(), ld, at["tokens"], n_tokens, ld_tokens,
+                    _vector(token_count, "token_count", row, i32, dev),
+                    _vector(repetition, "repetition", row, f32, dev),
+                    _vector(presence, "presence", row, f32, dev),
+                    _vector(frequency, "frequency", row, f32, dev), at["bias_index"],
+                    at["bias_value"], n_bias, ld_bias, at["mask"], n_masks,
+                    _vector(mask_row, "mask_row", row, i32, dev))
     L = load_library()
-    with _OnStream(logits, stream) as on:
+
+    def call(handle):
         if out is None:
-            out = torch.empty((rows, V), dtype=out_dtype or logits.dtype, device=dev)
-        elif out_dtype is not None and out.dtype != out_dtype:
-            raise ValueError(f"out: expected {out_dtype}")
-        ld_out = _matrix(out, "out", logits)
-        a = _AdjustArgs(rows, V, _elem(logits.dtype), _opt(logits), ld, _opt(tokens), n_tokens,
-                        ld_tokens, _opt(token_count), _opt(repetition), _opt(presence),
-                        _opt(frequency), _opt(bias_index), _opt(bias_value), n_bias, ld_bias,
-                        _opt(mask), n_masks, _opt(mask_row))
-        _check(L.hbsjd_adjust_rows(
-            ctypes.byref(a), _opt(out), _elem(out.dtype), ld_out,
-            on.uses(logits, tokens, token_count, repetition, presence, frequency, bias_index,
-                    bias_value, mask, mask_row, out)), "hbsjd_adjust_rows")
-    return out
+            o = logits.new_empty((rows, V), dtype=out_dtype)
+            ld_out = V
+        else:
+            o = out
+            ld_out = _matrix(o, "out", logits)[2]
+            if out_dtype is not None and o.dtype is not out_dtype:
+                raise ValueError(f"out: expected {out_dtype}")
+        _check(L.hbsjd_adjust_rows(ctypes.byref(a), o.data_ptr(), _elem(o.dtype), ld_out, handle),
+               "hbsjd_adjust_rows")
+        return o
+
+    return _on_stream(call, dev, stream,
+                      (logits, tokens, token_count, repetition, presence, frequency, bias_index,
+                       bias_value, mask, mask_row, out))
 
 
 def hbsjd_mfma_probe(workgroups: int, iters: int, sink, stream=None):
