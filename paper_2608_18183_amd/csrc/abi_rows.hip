@@ -117,8 +117,13 @@ hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* p, float* loss, vo
         if (const char* why = workspace_problem(
                 workspace, workspace_bytes, distill_top_workspace(p->rows, p->V, p->K, p->elem)))
             return api_fail(HBSJD_EINVAL, why);
+        const double log2_tau = 1.4426950408889634074 / (double)p->temperature;
+        float log2_hi = (float)log2_tau;   // rounded down: the rest is positive
+        if ((double)log2_hi >= log2_tau) log2_hi = std::nextafterf(log2_hi, 0.f);
+        const float log2_lo = (float)(log2_tau - (double)log2_hi);
         DistillArgs a{p->rows, p->V, p->K, p->logits, p->elem, p->ld, p->values, p->index, p->rest,
-                      1.f / p->temperature, alpha, beta, p->row_weight, loss, grad, ld_grad};
+                      1.f / p->temperature, 1.0 / p->temperature, make_float2(log2_hi, log2_lo),
+                      alpha, beta, p->row_weight, loss, grad, ld_grad};
         distill_top(a, workspace, (hipStream_t)stream);
         return launched("distill_top_rows");
     } catch (...) {

@@ -21,7 +21,7 @@ namespace hbsjd {
 namespace {
 
 constexpr float kNan = __builtin_nanf("");
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // What a workgroup of NT threads works out about a row once the row's unlisted
 // maximum is known; the same for every way the row itself is held.
@@ -29,7 +29,7 @@ struct Entries {
     uint32_t* listed;   // a bit per entry, in the order of the row's vectors
     int* entry;         // [K] the listed entries, -1 unused
     float* zk;          // [K] the student's logits there
-    float* tk;          // [K] the teacher's / tau
+    float* tk;          // [K] the teacher's
     __device__ __forceinline__ static Entries in(void* lds, int V, int K) {
         Entries e;
         e.listed = (uint32_t*)lds;
@@ -53,7 +53,7 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
     const int32_t* ti = a.index + r * a.K;
     for (int k = threadIdx.x; k < a.K; k += NT) {
         int v = ti[k];
-        const float x = tv[k] * a.inv_tau;
+        const float x = tv[k];
         if (v < 0 || v >= a.V) {
             if (v != -1) *bad = 1;
             v = -1;
@@ -72,7 +72,7 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
             if (!gather || !gathered) {
                 e.zk[k] = y;
                 mk = fmaxf(mk, y);
-                mt = fmaxf(mt, x);
+                mt = fmaxf(mt, x * a.inv_tau);
             }
         }
         e.entry[k] = v;
@@ -80,56 +80,89 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
     }
 }
 
+// exp of a number held in 64 bits, to a rounding or two of fp32: the hardware's
+// exp2 takes 32 bits, the argument's own rounding is put back to first order
+__device__ __forceinline__ float exp_of(double x) {
+    const double u = x * 1.4426950408889634074;
+    const float h = (float)u;
+    const float e = __builtin_amdgcn_exp2f(h);
+    return h < -200.f ? 0.f : fmaf(e, (float)(u - (double)h) * kLn2, e);
+}
+
 struct RowStats {
-    float m, lz, lt, rsum, loss, factor;   // factor: of e_v in the unlisted gradient
+    float less;     // R, and what the listed entries' c have of D too much
+    float loss;
+    float factor;   // of e_v in the unlisted gradient
     bool ok;
 };
 
-// everything but the row's own sum: from the maxima (block-wide) and this
-// thread's part of s_0
+// Everything but the row's own sum: from the maxima (block-wide) and this
+// thread's part of s_0. With a = log P and b = log q up to their normalisers'
+// logs, an entry's c is b - a - D, D the difference of those logs. A loss far
+// below the logs it is made of keeps its digits: a and b are differences in 64
+// bits, c is formed with any D_f near D, the sums of P c and q c are held in 64
+// bits, and D - D_f, which every entry shares, joins them at the end. One
+// wavefront works out the logs in 64 bits; the exponentials are fp32's.
+// Leaves alpha (q - P) + beta q c in zk and beta q in tk for listed_gradient().
 template <int NT>
 __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries& e, float rest, float m0,
                                             float mk, float mt, float s0_part, bool bad,
-                                            float (*red)[NT / 64], float (*red2)[NT / 64]) {
-    RowStats w;
-    w.m = fmaxf(m0, mk);
+                                            float (*red)[NT / 64], double (*red2)[NT / 64],
+                                            double* shared) {
+    const float m = fmaxf(m0, mk);
+    auto student = [&](float z) { return ((double)z - (double)m) * a.inv_tau_d; };
+    auto teacher = [&](float t) { return (double)t * a.inv_tau_d - (double)mt; };
     float s[3] = {s0_part, 0.f, 0.f};
     for (int k = threadIdx.x; k < a.K; k += NT) {
         if (e.entry[k] < 0) continue;
-        s[1] += __expf((e.zk[k] - w.m) * a.inv_tau);
-        s[2] += __expf(e.tk[k] - mt);
+        s[1] += exp_of(student(e.zk[k]));
+        s[2] += exp_of(teacher(e.tk[k]));
     }
     block_all<NT, 3>(s, red, AddOp());
-    const float s0 = s[0], st = a.rest ? s[2] + __expf(rest - mt) : s[2];
-    const float sz = s0 * __expf((m0 - w.m) * a.inv_tau) + s[1];
-    // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or NaN)
-    const bool some = sz > 0.f && st > 0.f;
-    w.lz = __logf(sz);
-    w.lt = mt + __logf(st);
-    float d[2] = {0.f, 0.f};   // sum P (log P - log q), sum q (log q - log P)
+    const double b0_ref = student(m0), a0 = (double)rest - (double)mt;
+    const float s0 = s[0], s0m = s0 * exp_of(b0_ref);
+    const float rest_e = a.rest ? exp_of(a0) : 0.f;
+    const float sz = s0m + s[1], st = s[2] + rest_e;
+    const float iz = 1.f / sz, it = 1.f / st;
+    const float D_f = __logf(sz) - __logf(st);
+    const float q0 = s0m * iz, p0 = rest_e * it;
+    const bool reverse = a.beta > 0.f;   // else its sums may be infinite, and count for nothing
+    double d[2] = {0.0, 0.0};   // sum P (log P - log q), sum q (log q - log P)
     for (int k = threadIdx.x; k < a.K; k += NT) {
         if (e.entry[k] < 0) continue;
-        const float lp = e.tk[k] - w.lt, lq = (e.zk[k] - w.m) * a.inv_tau - w.lz;
-        const float p = __expf(lp), q = __expf(lq), c = lq - lp;
-        if (p > 0.f) d[0] -= p * c;
-        if (q > 0.f) d[1] += q * c;
+        const double b = student(e.zk[k]), t = teacher(e.tk[k]), c = b - t - (double)D_f;
+        const float p = exp_of(t) * it, q = exp_of(b) * iz;
+        if (p > 0.f) d[0] -= (double)p * c;
+        if (q > 0.f) d[1] += (double)q * c;
+        e.zk[k] = a.alpha * (q - p) + (reverse && q > 0.f ? a.beta * q * (float)c : 0.f);
+        e.tk[k] = a.beta * q;
+    }
+    if (threadIdx.x < 64) {
+        const double D = log((double)sz / (double)st);
+        const double c = a.rest ? b0_ref + log((double)s0) - a0 : 0.0;   // of the others, + D
+        if (threadIdx.x == 0) {
+            if (a.rest) {
+                if (p0 > 0.f) d[0] -= (double)p0 * (c - (double)D_f);
+                if (q0 > 0.f) d[1] += (double)q0 * (c - (double)D_f);
+            }
+            shared[0] = D - (double)D_f;
+            shared[1] = c - D;
+        }
     }
     block_all<NT, 2>(d, red2, AddOp());
-    const float lq0 = (m0 - w.m) * a.inv_tau + __logf(s0) - w.lz, q0 = __expf(lq0);
-    float f = a.alpha * q0;
-    if (a.rest) {
-        const float lp = rest - w.lt, p = __expf(lp), c = lq0 - lp;
-        if (p > 0.f) d[0] -= p * c;
-        if (q0 > 0.f) d[1] += q0 * c;
-        f -= a.alpha * p;
-        if (a.beta > 0.f && q0 > 0.f) f += a.beta * q0 * (c - d[1]);
-    }
-    w.factor = s0 > 0.f ? f / s0 : 0.f;
-    w.rsum = d[1];
-    w.loss = a.alpha > 0.f ? a.alpha * d[0] : 0.f;
-    if (a.beta > 0.f) w.loss += a.beta * d[1];
-    if (bad || !some) w.loss = kNan;
+    if (NT == 64) __syncthreads();
+    const double late = shared[0];
+    const float R = reverse ? (float)(d[1] - late) : 0.f;
+    RowStats w;
+    w.loss = (float)((a.alpha > 0.f ? a.alpha * (d[0] + late) : 0.0) +
+                     (reverse ? a.beta * (d[1] - late) : 0.0));
+    // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or NaN)
+    if (bad || !(sz > 0.f && st > 0.f)) w.loss = kNan;
     w.ok = w.loss > -INFINITY && w.loss < INFINITY;
+    float f = a.alpha * (q0 - p0);
+    if (reverse && q0 > 0.f) f += a.beta * q0 * ((float)shared[1] - R);
+    w.factor = s0 > 0.f ? f / s0 : 0.f;
+    w.less = R + (float)late;
     return w;
 }
 
@@ -140,11 +173,7 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Entr
     for (int k = threadIdx.x; k < a.K; k += NT) {
         const int v = e.entry[k] - first;
         if (e.entry[k] < 0 || v < 0 || v >= V) continue;
-        const float lp = e.tk[k] - w.lt, lq = (e.zk[k] - w.m) * a.inv_tau - w.lz;
-        const float p = __expf(lp), q = __expf(lq);
-        float d = a.alpha * (q - p);
-        if (a.beta > 0.f && q > 0.f) d += a.beta * q * (lq - lp - w.rsum);
-        g[v] = narrow<T>(wt * d);
+        g[v] = narrow<T>(wt * (e.zk[k] - e.tk[k] * w.less));
     }
 }
 
@@ -159,6 +188,13 @@ __device__ __forceinline__ void fill_row(T* g, int V, float x) {
     u32x4* g4 = (u32x4*)(g + sp.head);
     for (int j = threadIdx.x; j < sp.vecs; j += NT) g4[j] = raw;
     if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(x);
+}
+
+// exp(d / tau): log2 e / tau in two parts, since the rounding of one alone would
+// put all entries of the sum off the same way. (Both are positive: d = -infinity
+// gives 0.)
+__device__ __forceinline__ float power(float d, float2 c2) {
+    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
 }
 
 // ---- a row, or a part of one, in registers: NV 16-byte vectors a thread
@@ -205,23 +241,23 @@ template <typename T, int NT, int NV> struct Held {
     }
     // x becomes exp2((x - m0) c2) in fp32 rows (16-bit ones keep the logits, and
     // work the exponentials out again when they are stored: half the registers)
-    __device__ __forceinline__ float sum(float m0, float c2) {
+    __device__ __forceinline__ float sum(float m0, float2 c2) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int q = 0; q < E; ++q) {
-                const float y = __builtin_amdgcn_exp2f((vec_get<T>(x[i], q) - m0) * c2);
+                const float y = power(vec_get<T>(x[i], q) - m0, c2);
                 s += y;
                 if constexpr (E == 4) x[i][q] = __float_as_uint(y);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        xe = __builtin_amdgcn_exp2f((xe - m0) * c2);
+        xe = power(xe - m0, c2);
         return s + xe;
     }
     // f times the exponentials, after sum()
-    __device__ __forceinline__ void store(T* g, const T* z, int V, float f, float m0, float c2) {
+    __device__ __forceinline__ void store(T* g, const T* z, int V, float f, float m0, float2 c2) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
@@ -233,7 +269,7 @@ template <typename T, int NT, int NV> struct Held {
 #pragma unroll
             for (int q = 0; q < E; ++q) {
                 if constexpr (E == 4) y[q] = f * __uint_as_float(x[i][q]);
-                else y[q] = f * __builtin_amdgcn_exp2f((vec_get<T>(x[i], q) - m0) * c2);
+                else y[q] = f * __builtin_amdgcn_exp2f((vec_get<T>(x[i], q) - m0) * c2.x);
             }
             __builtin_amdgcn_sched_barrier(0);
             if (j >= sp.vecs) continue;
@@ -248,19 +284,20 @@ template <typename T, int NT, int NV> struct Held {
     }
 };
 
-constexpr int waves_of(int nv) { return nv > 8 ? 4 : 5; }
+constexpr int waves_of(int nt) { return nt == 1024 ? 4 : 5; }
 
 // A workgroup of NT threads per row: logits leave memory once. The gradient at
 // the listed entries is stored over the row's afterwards.
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)))) void k_distill(
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_distill(
     DistillArgs a, int64_t r0) {
     extern __shared__ uint32_t lds[];
-    __shared__ float red[8][NT / 64];
+    __shared__ float red[6][NT / 64];
+    __shared__ double red2[2][NT / 64], shared[2];
     __shared__ int bad;
     const int t = threadIdx.x;
     const Entries e = Entries::in(lds, a.V, a.K);
-    const float c2 = a.inv_tau * kLog2e;
+    const float2 c2 = a.log2_tau;
     const int64_t r = r0 + blockIdx.x;
     const T* z = (const T*)a.logits + r * a.ld;
     T* g = a.grad ? (T*)a.grad + r * a.ld_grad : nullptr;
@@ -283,7 +320,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)
     block_all<NT, 3>(mm, red, MaxOp());
     const float m0 = mm[0] == -INFINITY ? fmaxf(mm[1], mm[0]) : mm[0];
     const float s0 = h.sum(m0, c2);
-    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s0, bad != 0, red + 3, red + 6);
+    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s0, bad != 0, red + 3, red2, shared);
     if (a.loss && t == 0) a.loss[r] = w * st.loss;
     if (g && !st.ok) fill_row<NT>(g, a.V, kNan);
     if (g && st.ok) {
@@ -307,14 +344,15 @@ struct PartsArgs {
 };
 
 template <typename T, int NT, int NV, bool Second>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)))) void k_distill_part(
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_distill_part(
     DistillArgs a, PartsArgs p, int64_t r0) {
     extern __shared__ uint32_t lds[];
-    __shared__ float red[8][NT / 64];
+    __shared__ float red[6][NT / 64];
+    __shared__ double red2[2][NT / 64], shared[2];
     __shared__ int bad;
     const int t = threadIdx.x;
     const Entries e = Entries::in(lds, p.len, a.K);
-    const float c2 = a.inv_tau * kLog2e;
+    const float2 c2 = a.log2_tau;
     const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
     const int64_t r = r0 + row;
     const int first = c * p.len, V = min(p.len, a.V - first);
@@ -360,10 +398,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NV)
         if (m0 == -INFINITY) m0 = mm[1];
         for (int i = 0; i < p.parts; ++i) {
             const float m = stats[3 * i], s = stats[3 * i + 1];
-            s0 += m == -INFINITY ? s : s * __builtin_amdgcn_exp2f((m - m0) * c2);
+            s0 += m == -INFINITY ? s : s * power(m - m0, c2);
         }
         const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], t == 0 ? s0 : 0.f, refused, red + 3,
-                                        red + 6);
+                                        red2, shared);
         if (a.loss && c == 0 && t == 0) a.loss[r] = w * st.loss;
         if (!g) return;
         if (!st.ok) {

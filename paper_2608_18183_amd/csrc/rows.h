@@ -122,27 +122,41 @@ template <int Ctrl, int RowMask> __device__ __forceinline__ float dpp_or(float v
     return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(v), Ctrl,
                                                       RowMask, 0xF, false));
 }
+template <int Ctrl, int RowMask> __device__ __forceinline__ double dpp_or(double v, double other) {
+    const uint2 x = __builtin_bit_cast(uint2, v), o = __builtin_bit_cast(uint2, other);
+    return __builtin_bit_cast(
+        double, make_uint2(__builtin_amdgcn_update_dpp(o.x, x.x, Ctrl, RowMask, 0xF, false),
+                           __builtin_amdgcn_update_dpp(o.y, x.y, Ctrl, RowMask, 0xF, false)));
+}
+__device__ __forceinline__ float last_lane(float v) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ double last_lane(double v) {
+    const uint2 x = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(x.x, 63),
+                                                 __builtin_amdgcn_readlane(x.y, 63)));
+}
 struct MaxOp {
     static constexpr float none = -INFINITY;
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 struct AddOp {
     static constexpr float none = 0.f;
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+    template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
-template <typename F> __device__ __forceinline__ float wave_all(float v, F op) {
-    v = op(v, dpp_or<0x111, 0xF>(v, F::none));   // row_shr 1, 2, 4, 8: lane 15 of a row has its row
-    v = op(v, dpp_or<0x112, 0xF>(v, F::none));
-    v = op(v, dpp_or<0x114, 0xF>(v, F::none));
-    v = op(v, dpp_or<0x118, 0xF>(v, F::none));
-    v = op(v, dpp_or<0x142, 0xA>(v, F::none));   // row_bcast 15 and 31: lane 63 has all
-    v = op(v, dpp_or<0x143, 0xC>(v, F::none));
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+template <typename V, typename F> __device__ __forceinline__ V wave_all(V v, F op) {
+    v = op(v, dpp_or<0x111, 0xF>(v, (V)F::none));   // row_shr 1, 2, 4, 8: lane 15 of a row has its row
+    v = op(v, dpp_or<0x112, 0xF>(v, (V)F::none));
+    v = op(v, dpp_or<0x114, 0xF>(v, (V)F::none));
+    v = op(v, dpp_or<0x118, 0xF>(v, (V)F::none));
+    v = op(v, dpp_or<0x142, 0xA>(v, (V)F::none));   // row_bcast 15 and 31: lane 63 has all
+    v = op(v, dpp_or<0x143, 0xC>(v, (V)F::none));
+    return last_lane(v);
 }
 // N block-wide reductions with one barrier, for blocks of NT threads. The caller
 // puts a barrier before the same `red` is used again.
-template <int NT, int N, typename F>
-__device__ __forceinline__ void block_all(float (&v)[N], float (*red)[NT / 64], F op) {
+template <int NT, int N, typename V, typename F>
+__device__ __forceinline__ void block_all(V (&v)[N], V (*red)[NT / 64], F op) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_all(v[i], op);
     if constexpr (NT > 64) {
@@ -152,7 +166,7 @@ __device__ __forceinline__ void block_all(float (&v)[N], float (*red)[NT / 64], 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float r[NT / 64];
+            V r[NT / 64];
 #pragma unroll
             for (int w = 0; w < NT / 64; ++w) r[w] = red[i][w];
 #pragma unroll
@@ -205,7 +219,10 @@ struct DistillArgs {
     const float* values;    // [rows][K]
     const int32_t* index;   // [rows][K]
     const float* rest;      // [rows] or null
-    float inv_tau, alpha, beta;
+    float inv_tau;
+    double inv_tau_d;
+    float2 log2_tau;        // log2 e / temperature in two parts
+    float alpha, beta;
     const float* weight;    // [rows] or null
     float* loss;            // [rows] or null
     void* grad;             // [rows], stride ld_grad, or null

@@ -273,6 +273,44 @@ def test_distill_masks_of_the_lowest_value_and_far_tails():
         check_distill(x64, values, index, rest, w, 1.0, 0.7, 0.3, loss, grad, dtype)
 
 
+@pytest.mark.parametrize("V", [300, 20000])
+def test_distill_forward_alone_with_entries_of_no_mass(V):
+    """Listed entries at -infinity on the teacher's side and a rest of no mass
+    leave the forward divergence and its gradient finite."""
+    rng = np.random.default_rng(V)
+    n, k = 3, 6
+    x = rng.normal(0, 2, (n, V)).astype(np.float32)
+    values, index, rest = teacher_of(rng, x.astype(np.float64), k, 1.0)
+    values[0, 4], values[1, 5], rest[1], rest[2] = -np.inf, -np.inf, -np.inf, -200.0
+    for r_ in (rest, None):
+        loss, grad = P().hbsjd_distill_top_rows(
+            dev(x), dev(values), dev(index), None if r_ is None else dev(r_), forward_weight=1.5,
+            reverse_weight=0.0)
+        assert bool(torch.isfinite(loss).all())
+        check_distill(x.astype(np.float64), values, index, r_, np.ones(n), 1.0, 1.5, 0.0, loss, grad,
+                      "f32")
+
+
+@pytest.mark.parametrize("tau", [0.7, 1.0, 3.0])
+def test_distill_of_nearly_equal_rows_keeps_its_digits(tau):
+    """A student close to its teacher: the loss is far below the logs it is made
+    of. Exponentials good to 2^-22 put q_0 and the entries' q off by that much, to
+    which the divergence of near rows is sensitive by |q - P| and |log q - log P|;
+    the inputs' own rounding is part of the reference."""
+    rng = np.random.default_rng(5)
+    n, V, k = 6, 16384, 64
+    x = (rng.normal(0, 1, (n, V)) + 20).astype(np.float32)
+    values, index, rest = teacher_of(rng, x.astype(np.float64), k, tau, noise=1e-2)
+    loss, grad = P().hbsjd_distill_top_rows(dev(x), dev(values), dev(index), dev(rest), temperature=tau)
+    for r in range(n):
+        wl, wg, _, _ = ref.distill(x[r].astype(np.float64), values[r].astype(np.float64), index[r],
+                                   np.float64(rest[r]), 1.0, tau, 0.5, 0.5)
+        # |c| is at most about 0.05 / tau here, sum |q - P| and sum (P + q) |c|
+        # below 0.05; each rounding above meets one of them, and rest, rounded at
+        # about 30 / tau, shifts log P_0 by half an fp32 step of it (in the input)
+        assert abs(float(loss[r]) - wl) <= 0.05 * (2.0 ** -22 * 4) + 2.0 ** -22 * wl
+
+
 def test_distill_over_all_entries_is_the_bidirectional_divergence():
     """With every entry listed the loss is the one hbsjd_bikl_rows computes."""
     rng = np.random.default_rng(9)
