@@ -46,8 +46,8 @@ __device__ __forceinline__ int index_of(uint64_t c) { return (int)~(uint32_t)c; 
 __device__ __forceinline__ float logit_of(uint64_t c) { return value_of((uint32_t)(c >> 32)); }
 
 // room for candidates
-inline int top_cap(int K) { return K <= 256 ? 1024 : 4096; }
-inline size_t top_lds(int cap) { return (size_t)cap * 10 + (kBins + 1) * 4; }
+constexpr int kFew = 1024, kMany = 4096;
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 // Where a row's entries come from and its results go: a row of logits, or the
 // lists of a row's parts, whose entry v stands for entry map[v] and to whose
@@ -166,15 +166,13 @@ template <int NV> __device__ __forceinline__ void opaque(u32x4 (&x)[NV]) {
     for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
 }
 
-template <typename T, int NT, int NV>
-__device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out,
-                                        int cap) {
+template <typename T, int NT, int NV, int Cap>
+__device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out) {
     constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
     static_assert(N >= 8, "eight groups a thread");
-    extern __shared__ uint64_t cand[];
-    int* bins = (int*)(cand + cap);
-    uint16_t* perm = (uint16_t*)(bins + kBins + 1);
-    __shared__ float red[4][NW];
+    __shared__ __attribute__((aligned(16))) uint64_t cand[Cap + 8];
+    __shared__ int bins[kBins];
+    __shared__ float red[5][NW];
     __shared__ int s_count[NW];
     __shared__ int word[4];
     __shared__ float s_last;
@@ -281,7 +279,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         C += s_count[w];
         below += red[1][w];
     }
-    if (C > cap || C < K || below != below) {
+    if (C > Cap || C < K || below != below) {
         __syncthreads();
         top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
         return;
@@ -298,94 +296,119 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     if (xe >= from) cand[slot++] = ranked(xe, sp.edge(t, V));
 
     // ---- 3. places
+    constexpr int M = Cap / NT;   // candidates a thread looks after
+    static_assert(M >= 1 && M * NT == Cap, "");
+    uint64_t me[M];
+    int place[M];                 // K where it is known only not to be lower
     if (C <= kPairs) {
+        // zeros, below every candidate, to a whole number of steps
+        if (t < 8) cand[C + t] = 0;
         __syncthreads();
-        for (int c = t; c < C; c += NT) {
-            const uint64_t me = cand[c];
-            int place = 0;
-            for (int j = 0; j < C; ++j) place += cand[j] > me;
-            if (place < K) out.put(place, me);
-            if (place == K - 1) s_last = logit_of(me);
-            perm[c] = place;
+#pragma unroll
+        for (int n = 0; n < M; ++n) {
+            const int c = t + NT * n;
+            me[n] = 0;
+            place[n] = K;
+            if (n * NT >= kPairs || c >= C) continue;
+            me[n] = cand[c];
+            int p = 0;
+            for (int j = 0; j < C; j += 8)
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const u64x2 pair = *(const u64x2*)(cand + j + i);
+                    p += (pair.x > me[n]) + (pair.y > me[n]);
+                }
+            place[n] = p;
+            if (p < K) out.put(p, me[n]);
+            if (p == K - 1) s_last = logit_of(me[n]);
         }
         __syncthreads();
     } else {
-        for (int i = t; i <= kBins; i += NT) bins[i] = 0;
-        if (t == 0) {
-            word[0] = -1;   // as unsigned: least image
-            word[1] = 0;    // largest
-            word[2] = 0;    // most entries in a bin
-        }
+        for (int i = t; i < kBins; i += NT) bins[i] = 0;
+        if (t == 0) word[2] = 0;   // most entries in a bin
         __syncthreads();
-        uint32_t least = 0xFFFFFFFFu, most = 0;
-        for (int c = t; c < C; c += NT) {
-            const uint32_t k = cand[c] >> 32;
-            least = min(least, k);
-            most = max(most, k);
+        float ends[2] = {-INFINITY, -INFINITY};   // of the candidates: least, negated, and largest
+#pragma unroll
+        for (int n = 0; n < M; ++n) {
+            const int c = t + NT * n;
+            me[n] = c < C ? cand[c] : 0;
+            if (c < C) {
+                ends[0] = fmaxf(ends[0], -logit_of(me[n]));
+                ends[1] = fmaxf(ends[1], logit_of(me[n]));
+            }
         }
-        atomicMin((uint32_t*)&word[0], least);
-        atomicMax((uint32_t*)&word[1], most);
-        __syncthreads();
-        least = word[0];
-        most = word[1];
-        const float lo = value_of(least), hi = value_of(most);
+        block_all<NT, 2>(ends, &red[2], MaxOp());
+        const float lo = -ends[0], hi = ends[1];
+        const uint32_t least = order_of(lo), most = order_of(hi);
         // Bins on the images where all candidates have one sign: even an outlier
         // among them only costs some octaves. Across zero, where the images of
         // small numbers would take most bins, on the logits themselves.
         const bool images = (least ^ most) >> 31 == 0 || !(hi - lo < INFINITY);
         const int shift = max(22 - __clz((int)(most - least)), 0);
         const float scale = (kBins - 1) / (hi - lo);
-        auto bin_of = [&](uint64_t c) {
+        auto bin_of = [&](uint64_t c) {   // from the largest down
             const uint32_t k = c >> 32;
-            // from the largest down
             const int b = images ? (int)((k - least) >> shift) : (int)((value_of(k) - lo) * scale);
             return kBins - 1 - min(max(b, 0), kBins - 1);
         };
-        for (int c = t; c < C; c += NT) atomicAdd(&bins[bin_of(cand[c])], 1);
+#pragma unroll
+        for (int n = 0; n < M; ++n)
+            if (t + NT * n < C) atomicAdd(&bins[bin_of(me[n])], 1);
         __syncthreads();
         // exclusive prefix sums: thread t has its consecutive bins
-        constexpr int B = kBins / NT > 0 ? kBins / NT : 1;
+        constexpr int B = kBins / NT;
         int own[B], sum = 0, big = 0;
-        if (t * B < kBins)
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                own[b] = bins[t * B + b];
-                sum += own[b];
-                big = max(big, own[b]);
-            }
+        for (int b = 0; b < B; ++b) {
+            own[b] = bins[t * B + b];
+            sum += own[b];
+            big = max(big, own[b]);
+        }
         int all;
         int start = wave_prefix(sum, all);
         if (lane == 0) s_count[wv] = all;
-        atomicMax(&word[2], big);
+        if (big > kBinMost) word[2] = 1;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < NW; ++w)
             if (w < wv) start += s_count[w];
-        if (word[2] > kBinMost) {
+        if (word[2]) {
             __syncthreads();
             top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
             return;
         }
-        if (t * B < kBins)
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                bins[t * B + b] = start;
-                start += own[b];
-            }
-        __syncthreads();
-        // candidates by bin; afterwards bins[b] is where bin b + 1 starts
-        for (int c = t; c < C; c += NT) perm[atomicAdd(&bins[bin_of(cand[c])], 1)] = c;
-        __syncthreads();
-        for (int c = t; c < C; c += NT) {
-            const uint64_t me = cand[c];
-            const int b = bin_of(me), from_ = b ? bins[b - 1] : 0, to = bins[b];
-            if (from_ >= K) continue;
-            int place = from_;
-            for (int j = from_; j < to; ++j) place += cand[perm[j]] > me;
-            if (place < K) out.put(place, me);
-            if (place == K - 1) s_last = logit_of(me);
+        for (int b = 0; b < B; ++b) {
+            bins[t * B + b] = start;
+            start += own[b];
         }
         __syncthreads();
+        // the candidates by bin, in the list's place; afterwards bins[b] is where
+        // bin b + 1 starts
+#pragma unroll
+        for (int n = 0; n < M; ++n)
+            if (t + NT * n < C) cand[atomicAdd(&bins[bin_of(me[n])], 1)] = me[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < M; ++n) {
+            place[n] = K;
+            if (t + NT * n >= C) continue;
+            const int b = bin_of(me[n]), first = b ? bins[b - 1] : 0, end = bins[b];
+            if (first >= K) continue;
+            int p = first;
+            for (int j = first; j < end; j += 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p += (j + i < end) & (cand[j + i] > me[n]);
+            place[n] = p;
+            if (p == K - 1) s_last = logit_of(me[n]);
+        }
+        __syncthreads();
+        // in order, for whole lines to be written
+#pragma unroll
+        for (int n = 0; n < M; ++n)
+            if (place[n] < K) cand[place[n]] = me[n];
+        __syncthreads();
+        for (int k = t; k < K; k += NT) out.put(k, cand[k]);
     }
 
     // ---- the mass of the others: below the pivot, and the candidates left over
@@ -398,32 +421,11 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     }
     float over = 0.f;
     if (C > K) {
-        // those whose place is K or more, in the order of the list
-        if (C <= kPairs) {
-            for (int c = t; c < C; c += NT)
-                if (perm[c] >= K) over += __builtin_amdgcn_exp2f((logit_of(cand[c]) - last) * c2);
-        } else {
-            // equal ones count the same whichever of them were taken
-            int taken = 0;
-            for (int c = t; c < C; c += NT) {
-                const uint32_t k = cand[c] >> 32;
-                if (k < last_image) over += __builtin_amdgcn_exp2f((value_of(k) - last) * c2);
-                taken += k >= last_image;
-            }
-            int n;
-            wave_prefix(taken, n);
-            if (lane == 0) s_count[wv] = n;
-        }
-        float o[1] = {over};
-        block_all<NT, 1>(o, &red[2], AddOp());
-        over = o[0];
-        if (C > kPairs) {
-            if (NT == 64) __syncthreads();
-            int n = 0;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) n += s_count[w];
-            over += (float)(n - K);
-        }
+        for (int n = 0; n < M; ++n)
+            if (t + NT * n < C && place[n] >= K)
+                over += __builtin_amdgcn_exp2f((logit_of(me[n]) - last) * c2);
+        over = block_all<NT>(over, red[2], AddOp());
     }
     // A sum too far below its reference: again, relative to the largest term.
     // (With candidates left over the mass below the pivot is at most V times the
@@ -442,7 +444,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
             const float y = widen(z[v]);
             s += ranked(y, 0) < bound && m > -INFINITY ? __builtin_amdgcn_exp2f((y - m) * c2) : 0.f;
         }
-        s = block_all<NT>(s, red[3], AddOp());
+        s = block_all<NT>(s, red[4], AddOp());
         ref_below = m;
         below = s;
         over = 0.f;
@@ -455,11 +457,11 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     }
 }
 
-template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_top(TopArgs a, int cap, int64_t r0) {
+template <typename T, int NT, int NV, int Cap>
+__global__ __launch_bounds__(NT) void k_top(TopArgs a, int64_t r0) {
     const int64_t r = r0 + blockIdx.x;
     const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0};
-    top_row<T, NT, NV>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out, cap);
+    top_row<T, NT, NV, Cap>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out);
 }
 
 // Long rows: every part's K largest and the mass of its others go to the
@@ -473,22 +475,22 @@ struct PartsArgs {
     float* rest;     // [rows of the slab][parts]
 };
 
-template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_top_part(TopArgs a, PartsArgs p, int cap, int64_t r0) {
+template <typename T, int NT, int NV, int Cap>
+__global__ __launch_bounds__(NT) void k_top_part(TopArgs a, PartsArgs p, int64_t r0) {
     const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
     const int first = c * p.len;
     const int64_t at = blockIdx.x;
     const TopRow out{p.values + at * a.K, p.index + at * a.K, p.rest + at, nullptr, nullptr, 0, first};
-    top_row<T, NT, NV>((const T*)a.logits + (r0 + row) * a.ld + first, min(p.len, a.V - first), a.K,
-                       a.inv_tau, out, cap);
+    top_row<T, NT, NV, Cap>((const T*)a.logits + (r0 + row) * a.ld + first, min(p.len, a.V - first), a.K,
+                            a.inv_tau, out);
 }
 
-template <int NT, int NV>
-__global__ __launch_bounds__(NT) void k_top_join(TopArgs a, PartsArgs p, int cap, int64_t r0) {
+template <int NT, int NV, int Cap>
+__global__ __launch_bounds__(NT) void k_top_join(TopArgs a, PartsArgs p, int64_t r0) {
     const int64_t row = blockIdx.x, r = r0 + row, n = (int64_t)p.parts * a.K;
     const TopRow out{a.values + r * a.K,  a.index + r * a.K, a.rest + r, p.index + row * n,
                      p.rest + row * p.parts, p.parts,           0};
-    top_row<float, NT, NV>(p.values + row * n, (int)n, a.K, a.inv_tau, out, cap);
+    top_row<float, NT, NV, Cap>(p.values + row * n, (int)n, a.K, a.inv_tau, out);
 }
 
 // How a call runs: whole rows, or in parts with workspace for `slab` rows.
@@ -506,7 +508,7 @@ Plan plan_of(int64_t rows, int V, int K) {
     Plan p;
     if (V <= kPart) return p;
     p.parts = (V + kPart - 1) / kPart;
-    while (rows * p.parts < 512 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
+    while (rows * p.parts < 256 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
         p.parts *= 2;
     p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (V + p.len - 1) / p.len;
@@ -515,30 +517,40 @@ Plan plan_of(int64_t rows, int V, int K) {
     return p;
 }
 
-// f(threads, vectors a thread) for the smallest workgroup that holds `vecs`
-// vectors and has groups enough for the pivot, or so few entries that all may be
-// candidates
-template <int NT, int NV, typename F> bool try_size(int vecs, int V, int K, F f) {
-    if (vecs > NT * NV || (NT * 8 < 2 * K && V > top_cap(K))) return false;
-    f(std::integral_constant<int, NT>{}, std::integral_constant<int, NV>{});
-    return true;
-}
-template <typename T, typename F> void by_size(int V, int K, F f) {
+// f(threads, vectors a thread, room for candidates) for the smallest workgroup of
+// at least `least` threads that holds the row. Up to K = 256 the maxima of 64
+// threads leave few enough candidates; a larger K takes workgroups with at least
+// 2 K groups, unless all of the row's entries may be candidates.
+template <typename T, typename F> void by_size(int V, int K, int least, F f) {
+    using std::integral_constant;
     const int vecs = V / kVec<T>;
-    if (try_size<64, 2>(vecs, V, K, f) || try_size<64, 8>(vecs, V, K, f) ||
-        try_size<256, 4>(vecs, V, K, f) || try_size<512, 4>(vecs, V, K, f))
-        return;
-    if constexpr (sizeof(T) == 4) try_size<512, 8>(vecs, V, K, f) || try_size<1024, 8>(vecs, V, K, f);
+    auto fits = [&](auto nt, auto nv) {
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        return NT >= least && vecs <= NT * NV && (NT * 8 >= 2 * K || V <= (NT == 64 ? kFew : kMany));
+    };
+#define FITS(nt, nv) fits(integral_constant<int, nt>{}, integral_constant<int, nv>{})
+#define CALL(nt, nv, cap) \
+    f(integral_constant<int, nt>{}, integral_constant<int, nv>{}, integral_constant<int, cap>{})
+    const bool few = K <= 256 || V <= kFew;
+    if (FITS(64, 2) && V <= kFew) CALL(64, 2, kFew);
+    else if (FITS(64, 8)) CALL(64, 8, kFew);
+    else if (FITS(256, 4)) { if (few) CALL(256, 4, kFew); else CALL(256, 4, kMany); }
+    else if (FITS(512, 4)) { if (few) CALL(512, 4, kFew); else CALL(512, 4, kMany); }
+    else if constexpr (sizeof(T) == 4) {
+        if (FITS(512, 8)) { if (few) CALL(512, 8, kFew); else CALL(512, 8, kMany); }
+        else CALL(1024, 8, kMany);
+    }
+#undef FITS
+#undef CALL
 }
 
 template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
-    const int cap = top_cap(a.K);
     const Plan plan = plan_of(a.rows, a.V, a.K);
     if (!plan.parts) {
-        by_size<T>(a.V, a.K, [&](auto nt, auto nv) {
-            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        by_size<T>(a.V, a.K, 64, [&](auto nt, auto nv, auto cap) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
             by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-                hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(NT), top_lds(cap), s, a, cap, r0);
+                hipLaunchKernelGGL((k_top<T, NT, NV, Cap>), grid, dim3(NT), 0, s, a, r0);
             });
         });
         return;
@@ -548,15 +560,16 @@ template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
     p.rest = (float*)(p.index + plan.slab * plan.parts * a.K);
     for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
         const int64_t n = std::min(plan.slab, a.rows - r0);
-        by_size<T>(p.len, a.K, [&](auto nt, auto nv) {
-            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((k_top_part<T, NT, NV>), dim3((unsigned)(n * p.parts)), dim3(NT),
-                               top_lds(cap), s, a, p, cap, r0);
+        by_size<T>(p.len, a.K, 256, [&](auto nt, auto nv, auto cap) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
+            if constexpr (NT >= 256 && NT <= 512)
+                hipLaunchKernelGGL((k_top_part<T, NT, NV, Cap>), dim3((unsigned)(n * p.parts)), dim3(NT),
+                                   0, s, a, p, r0);
         });
-        by_size<float>(p.parts * a.K, a.K, [&](auto nt, auto nv) {
-            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((k_top_join<NT, NV>), dim3((unsigned)n), dim3(NT), top_lds(cap), s, a, p,
-                               cap, r0);
+        by_size<float>(p.parts * a.K, a.K, 256, [&](auto nt, auto nv, auto cap) {
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
+            if constexpr (NT >= 256)
+                hipLaunchKernelGGL((k_top_join<NT, NV, Cap>), dim3((unsigned)n), dim3(NT), 0, s, a, p, r0);
         });
     }
 }
