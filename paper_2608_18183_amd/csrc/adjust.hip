@@ -237,10 +237,11 @@ template <typename T, typename O, int NT, int NV> void run(const AdjustArgs& a, 
     if (a.tokens) lds += (count_words(len, wide) + 3) / 4 * 4;
     if (a.n_bias) lds += (len + 31) / 32 + a.n_bias;
     if (a.mask) lds += len / 32 + 2;
+    lds = resident_lds(lds * 4, len * sizeof(T));
     by_slabs(
         a.rows,
         [&](int64_t r0, dim3 grid) {
-            hipLaunchKernelGGL((k_adjust<T, O, NT, NV>), grid, dim3(NT), lds * 4, s, a, parts, len, wide, r0);
+            hipLaunchKernelGGL((k_adjust<T, O, NT, NV>), grid, dim3(NT), lds, s, a, parts, len, wide, r0);
         },
         parts);
 }

@@ -151,7 +151,7 @@ __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries&
     }
     block_all<NT, 2>(d, red2, AddOp());
     if (NT == 64) __syncthreads();
-    const double late = shared[0];
+    const double late = uniform(shared[0]);
     const float R = reverse ? (float)(d[1] - late) : 0.f;
     RowStats w;
     w.loss = (float)((a.alpha > 0.f ? a.alpha * (d[0] + late) : 0.0) +
@@ -160,7 +160,7 @@ __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries&
     if (bad || !(sz > 0.f && st > 0.f)) w.loss = kNan;
     w.ok = w.loss > -INFINITY && w.loss < INFINITY;
     float f = a.alpha * (q0 - p0);
-    if (reverse && q0 > 0.f) f += a.beta * q0 * ((float)shared[1] - R);
+    if (reverse && q0 > 0.f) f += a.beta * q0 * ((float)uniform(shared[1]) - R);
     w.factor = s0 > 0.f ? f / s0 : 0.f;
     w.less = R + (float)late;
     return w;
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     block_all<NT, 3>(mm, red, MaxOp());
     const float m0 = mm[0] == -INFINITY ? fmaxf(mm[1], mm[0]) : mm[0];
     const float s0 = h.sum(m0, c2);
-    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s0, bad != 0, red + 3, red2, shared);
+    const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], s0, uniform(bad) != 0, red + 3, red2, shared);
     if (a.loss && t == 0) a.loss[r] = w * st.loss;
     if (g && !st.ok) fill_row<NT>(g, a.V, kNan);
     if (g && st.ok) {
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
             stats[3 * c + 2] = bad;
         }
     } else {
-        bool refused = bad != 0;
+        bool refused = uniform(bad) != 0;
         float m0 = -INFINITY, s0 = 0.f;
         for (int i = 0; i < p.parts; ++i) {
             m0 = fmaxf(m0, stats[3 * i]);
@@ -458,7 +458,8 @@ template <typename T> void go_parts(const DistillArgs& a, const Plan& plan, void
 template <typename T> void go(const DistillArgs& a, void* ws, hipStream_t s) {
     const Plan plan = plan_of(a.rows, a.V, a.K, a.elem);
     if (plan.parts) return go_parts<T>(a, plan, ws, s);
-    const size_t lds = entries_bytes(a.V, a.K);
+    size_t lds = entries_bytes(a.V, a.K);
+    if (a.grad) lds = resident_lds(lds, a.V * sizeof(T));
     const int vecs = a.V / kVec<T>;
     auto held = [&](auto nt, auto nv) {
         by_slabs(a.rows, [&](int64_t r0, dim3 grid) {

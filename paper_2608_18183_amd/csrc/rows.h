@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 #include <type_traits>
@@ -136,6 +137,17 @@ __device__ __forceinline__ double last_lane(double v) {
     return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(x.x, 63),
                                                  __builtin_amdgcn_readlane(x.y, 63)));
 }
+// a value that all lanes have, as one the compiler knows to be the same in all:
+// what follows from it is scalar, branches on it among them
+__device__ __forceinline__ float uniform(float v) {
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ double uniform(double v) {
+    const uint2 x = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readfirstlane(x.x),
+                                                 __builtin_amdgcn_readfirstlane(x.y)));
+}
 struct MaxOp {
     static constexpr float none = -INFINITY;
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
@@ -173,7 +185,7 @@ __device__ __forceinline__ void block_all(V (&v)[N], V (*red)[NT / 64], F op) {
             for (int n = NT / 128; n > 0; n /= 2)
 #pragma unroll
                 for (int w = 0; w < n; ++w) r[w] = op(r[w], r[w + n]);
-            v[i] = r[0];
+            v[i] = uniform(r[0]);
         }
     }
 }
@@ -192,6 +204,17 @@ template <typename F> inline void by_slabs(int64_t rows, F f, int parts = 1) {
     const int64_t slab = (1 << 21) / parts;
     for (int64_t r0 = 0; r0 < rows; r0 += slab)
         f(r0, dim3((unsigned)((rows - r0 < slab ? rows - r0 : slab) * parts)));
+}
+
+// LDS to ask for so that the workgroups of a CU, each of which reads `bytes` and
+// writes as much, read no more than the CU's share of the L2 (128 KB) between
+// them. With more of them, rows being read and rows being written displace one
+// another: divergence of 6144 fp32 rows of 16384, three and two workgroups a CU:
+// 164 and 153 us; 18432 bf16 rows, six and four: 237 and 219 (two: 278); 6400
+// adjusted fp32 rows, four and two: 168 and 159.
+inline size_t resident_lds(size_t lds, size_t bytes) {
+    const size_t groups = std::max<size_t>(2, (128 << 10) / bytes);
+    return std::max(lds, std::min<size_t>((160 << 10) / (groups + 1), 62 << 10));
 }
 
 // ------------------------------------------------------------ launchers

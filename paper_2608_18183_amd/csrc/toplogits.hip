@@ -25,7 +25,6 @@
 namespace hbsjd {
 namespace {
 
-constexpr int kBins = 1024;
 constexpr int kPairs = 256;      // candidates compared with all others
 constexpr int kBinMost = 256;    // entries of one bin
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -45,9 +44,48 @@ __device__ __forceinline__ uint64_t ranked(float x, int v) {
 __device__ __forceinline__ int index_of(uint64_t c) { return (int)~(uint32_t)c; }
 __device__ __forceinline__ float logit_of(uint64_t c) { return value_of((uint32_t)(c >> 32)); }
 
+// A candidate as one number: an order-preserving image of its logit above its
+// complemented index. 16-bit logits have 16-bit images, and with the 14 bits of
+// an index within a part the number takes 32 bits: half the LDS, and comparisons
+// at full rate (K = 2000 of 16384 bf16 entries, where equal logits share bins:
+// 54 us with 64 bits).
+constexpr int kPart = 16384;   // entries of a part at most
+template <typename T> struct Candidate {
+    using Key = uint64_t;
+    static constexpr int kBins = 1024;
+    __device__ __forceinline__ static Key of(float x, int v) { return ranked(x, v); }
+    __device__ __forceinline__ static int index(Key c) { return index_of(c); }
+    __device__ __forceinline__ static float logit(Key c) { return logit_of(c); }
+    // the image with what is worth binning by
+    __device__ __forceinline__ static uint32_t image(Key c) { return (uint32_t)(c >> 32); }
+    __device__ __forceinline__ static uint32_t least(float x) { return order_of(x); }
+    __device__ __forceinline__ static uint32_t most(float x) { return order_of(x); }
+};
+template <typename T> struct Candidate16 {
+    using Key = uint32_t;
+    static constexpr int kBins = 2048;
+    __device__ __forceinline__ static uint32_t order(float x) {
+        uint32_t u;
+        if constexpr (std::is_same_v<T, Bf16>) u = __float_as_uint(x + 0.f) >> 16;
+        else u = __builtin_bit_cast(uint16_t, (_Float16)(x + 0.f));
+        return u & 0x8000u ? ~u & 0xFFFFu : u | 0x8000u;
+    }
+    __device__ __forceinline__ static Key of(float x, int v) { return order(x) << 14 | (kPart - 1 - v); }
+    __device__ __forceinline__ static int index(Key c) { return kPart - 1 - (int)(c & (kPart - 1)); }
+    __device__ __forceinline__ static float logit(Key c) {
+        const uint32_t k = c >> 14, u = k & 0x8000u ? k & 0x7FFFu : ~k & 0xFFFFu;
+        if constexpr (std::is_same_v<T, Bf16>) return __uint_as_float(u << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
+    }
+    __device__ __forceinline__ static uint32_t image(Key c) { return c; }
+    __device__ __forceinline__ static uint32_t least(float x) { return order(x) << 14; }
+    __device__ __forceinline__ static uint32_t most(float x) { return order(x) << 14 | (kPart - 1); }
+};
+template <> struct Candidate<Bf16> : Candidate16<Bf16> {};
+template <> struct Candidate<F16> : Candidate16<F16> {};
+
 // room for candidates
 constexpr int kFew = 1024, kMany = 4096;
-typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 // Where a row's entries come from and its results go: a row of logits, or the
 // lists of a row's parts, whose entry v stands for entry map[v] and to whose
@@ -60,9 +98,9 @@ struct TopRow {
     const float* rests;
     int n_rests;
     int first;   // of the row's entries in the whole row
-    __device__ __forceinline__ void put(int k, uint64_t c) const {
-        values[k] = logit_of(c);
-        index[k] = map ? map[index_of(c)] : first + index_of(c);
+    __device__ __forceinline__ void put(int k, float x, int v) const {
+        values[k] = x;
+        index[k] = map ? map[v] : first + v;
     }
     // rest from the log of what the kernel itself left over
     __device__ __forceinline__ void put_rest(float own) const {
@@ -138,7 +176,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
             }
         }
     __syncthreads();
-    for (int k = t; k < K; k += NT) out.put(k, kept[k]);
+    for (int k = t; k < K; k += NT) out.put(k, logit_of(kept[k]), index_of(kept[k]));
     if (t == 0) {
         const bool nan = kept[0] >> 32 == 0xFFFFFFFFu;
         out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s));
@@ -170,7 +208,13 @@ template <typename T, int NT, int NV, int Cap>
 __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out) {
     constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
     static_assert(N >= 8, "eight groups a thread");
-    __shared__ __attribute__((aligned(16))) uint64_t cand[Cap + 8];
+    using Cand = Candidate<T>;
+    using Key = typename Cand::Key;
+    constexpr int kBins = Cand::kBins;
+    // (the digits' way keeps up to K 64-bit numbers there)
+    constexpr int kRoom = (Cap + 8) * (int)sizeof(Key), kKept = (Cap < HBSJD_TOP_MAX ? Cap : HBSJD_TOP_MAX) * 8;
+    __shared__ __attribute__((aligned(16))) char room[kRoom > kKept ? kRoom : kKept];
+    Key* cand = (Key*)room;
     __shared__ int bins[kBins];
     __shared__ float red[5][NW];
     __shared__ int s_count[NW];
@@ -236,6 +280,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < NW; ++w) p0 = fminf(p0, red[0][w]);
+            p0 = uniform(p0);
         }
     }
     // -infinity is nobody's candidate
@@ -279,9 +324,11 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         C += s_count[w];
         below += red[1][w];
     }
+    C = uniform(C);
+    below = uniform(below);
     if (C > Cap || C < K || below != below) {
         __syncthreads();
-        top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+        top_by_digits<NT>(z, V, K, inv_tau, out, (uint64_t*)room, bins, red[0], word);
         return;
     }
     opaque(x);
@@ -290,15 +337,15 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
         for (int q = 0; q < E; ++q) {
             const float y = vec_get<T>(x[i], q);
-            if (y >= from) cand[slot++] = ranked(y, sp.head + (t + NT * i) * E + q);
+            if (y >= from) cand[slot++] = Cand::of(y, sp.head + (t + NT * i) * E + q);
         }
     }
-    if (xe >= from) cand[slot++] = ranked(xe, sp.edge(t, V));
+    if (xe >= from) cand[slot++] = Cand::of(xe, sp.edge(t, V));
 
     // ---- 3. places
     constexpr int M = Cap / NT;   // candidates a thread looks after
     static_assert(M >= 1 && M * NT == Cap, "");
-    uint64_t me[M];
+    Key me[M];
     int place[M];                 // K where it is known only not to be lower
     if (C <= kPairs) {
         // zeros, below every candidate, to a whole number of steps
@@ -314,13 +361,15 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
             int p = 0;
             for (int j = 0; j < C; j += 8)
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const u64x2 pair = *(const u64x2*)(cand + j + i);
-                    p += (pair.x > me[n]) + (pair.y > me[n]);
+                for (int i = 0; i < 8; i += 16 / (int)sizeof(Key)) {
+                    typedef Key Vec __attribute__((ext_vector_type(16 / sizeof(Key))));
+                    const Vec other = *(const Vec*)(cand + j + i);
+#pragma unroll
+                    for (int q = 0; q < 16 / (int)sizeof(Key); ++q) p += other[q] > me[n];
                 }
             place[n] = p;
-            if (p < K) out.put(p, me[n]);
-            if (p == K - 1) s_last = logit_of(me[n]);
+            if (p < K) out.put(p, Cand::logit(me[n]), Cand::index(me[n]));
+            if (p == K - 1) s_last = Cand::logit(me[n]);
         }
         __syncthreads();
     } else {
@@ -333,22 +382,23 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
             const int c = t + NT * n;
             me[n] = c < C ? cand[c] : 0;
             if (c < C) {
-                ends[0] = fmaxf(ends[0], -logit_of(me[n]));
-                ends[1] = fmaxf(ends[1], logit_of(me[n]));
+                ends[0] = fmaxf(ends[0], -Cand::logit(me[n]));
+                ends[1] = fmaxf(ends[1], Cand::logit(me[n]));
             }
         }
         block_all<NT, 2>(ends, &red[2], MaxOp());
         const float lo = -ends[0], hi = ends[1];
-        const uint32_t least = order_of(lo), most = order_of(hi);
+        const uint32_t least = Cand::least(lo), most = Cand::most(hi);
         // Bins on the images where all candidates have one sign: even an outlier
         // among them only costs some octaves. Across zero, where the images of
         // small numbers would take most bins, on the logits themselves.
-        const bool images = (least ^ most) >> 31 == 0 || !(hi - lo < INFINITY);
-        const int shift = max(22 - __clz((int)(most - least)), 0);
+        const bool images = lo > 0.f || hi < 0.f || !(hi - lo < INFINITY);
+        constexpr int kBits = 31 - __builtin_clz(kBins);
+        const int shift = max(32 - kBits - __clz((int)(most - least)), 0);
         const float scale = (kBins - 1) / (hi - lo);
-        auto bin_of = [&](uint64_t c) {   // from the largest down
-            const uint32_t k = c >> 32;
-            const int b = images ? (int)((k - least) >> shift) : (int)((value_of(k) - lo) * scale);
+        auto bin_of = [&](Key c) {   // from the largest down
+            const int b = images ? (int)((Cand::image(c) - least) >> shift)
+                                 : (int)((Cand::logit(c) - lo) * scale);
             return kBins - 1 - min(max(b, 0), kBins - 1);
         };
 #pragma unroll
@@ -372,9 +422,9 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
         for (int w = 0; w < NW; ++w)
             if (w < wv) start += s_count[w];
-        if (word[2]) {
+        if (uniform(word[2])) {
             __syncthreads();
-            top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+            top_by_digits<NT>(z, V, K, inv_tau, out, (uint64_t*)room, bins, red[0], word);
             return;
         }
 #pragma unroll
@@ -400,7 +450,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p += (j + i < end) & (cand[j + i] > me[n]);
             place[n] = p;
-            if (p == K - 1) s_last = logit_of(me[n]);
+            if (p == K - 1) s_last = Cand::logit(me[n]);
         }
         __syncthreads();
         // in order, for whole lines to be written
@@ -408,15 +458,15 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         for (int n = 0; n < M; ++n)
             if (place[n] < K) cand[place[n]] = me[n];
         __syncthreads();
-        for (int k = t; k < K; k += NT) out.put(k, cand[k]);
+        for (int k = t; k < K; k += NT) out.put(k, Cand::logit(cand[k]), Cand::index(cand[k]));
     }
 
     // ---- the mass of the others: below the pivot, and the candidates left over
-    const float last = s_last;
+    const float last = uniform(s_last);
     const uint32_t last_image = order_of(last);
     if (last == INFINITY && C > K) {
         __syncthreads();
-        top_by_digits<NT>(z, V, K, inv_tau, out, cand, bins, red[0], word);
+        top_by_digits<NT>(z, V, K, inv_tau, out, (uint64_t*)room, bins, red[0], word);
         return;
     }
     float over = 0.f;
@@ -424,7 +474,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
         for (int n = 0; n < M; ++n)
             if (t + NT * n < C && place[n] >= K)
-                over += __builtin_amdgcn_exp2f((logit_of(me[n]) - last) * c2);
+                over += __builtin_amdgcn_exp2f((Cand::logit(me[n]) - last) * c2);
         over = block_all<NT>(over, red[2], AddOp());
     }
     // A sum too far below its reference: again, relative to the largest term.
@@ -498,8 +548,6 @@ struct Plan {
     int parts = 0, len = 0;
     int64_t slab = 0;
 };
-constexpr int kPart = 16384;   // entries of a part at most
-
 inline size_t part_row_bytes(const Plan& p, int K) { return (size_t)p.parts * (8 * (size_t)K + 4); }
 
 // Rows of more entries than a workgroup holds go in parts; where rows are few,
