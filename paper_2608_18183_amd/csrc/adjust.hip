@@ -8,25 +8,33 @@
 // A workgroup takes a part of a row. It counts the sequence's tokens that fall
 // into its part in LDS, so that an entry's count costs a fraction of a vector's
 // LDS access, and moves the logits through registers once, as 16-byte vectors.
-// Biased entries, which are few, are worked out one by one and stored over the
-// part's stores.
+// Biased entries are few: a thread works one out by itself and leaves the result
+// in LDS, with a tag in place of the entry's count. (Storing such entries over
+// the part's vectors instead costs more than the vectors' arithmetic: 4224 bf16
+// rows with 64 biases took 12 us longer, and 6400 fp32 rows whose penalties were
+// stored that way 40.)
 #include "rows.h"
 
 #include <algorithm>
+
+static_assert((HBSJD_ADJUST_MAX_BIASES & (HBSJD_ADJUST_MAX_BIASES - 1)) == 0, "a place in the list is a tag's low bits");
 
 #pragma clang fp contract(off)
 
 namespace hbsjd {
 namespace {
 
-// LDS of a workgroup: 16-bit counts of its entries (32-bit ones where a row may
-// hold more than 65535 tokens), a bit per biased entry, the mask's words
+// LDS of a workgroup: counts or tags of its entries, 16 bits each (32 where a row
+// may hold more tokens than 15 bits count); the mask's words; the bias list's
+// entries and what becomes of them
 struct AdjustLds {
     uint32_t* count;
-    uint32_t* biased;
+    uint32_t* biased;   // a bit per entry
     uint32_t* mask;
     int32_t* list;
+    float* result;
 };
+constexpr int kCountMost = 32767;
 inline __host__ __device__ int count_words(int len, bool wide) { return wide ? len : (len + 1) / 2; }
 
 struct Penalties {
@@ -55,7 +63,7 @@ __device__ __forceinline__ void store_vec(O* o, const float* y, int n, bool alig
     }
 }
 
-template <typename T, typename O, int NT, int NV>
+template <typename T, typename O, int NT, int NV, bool Biased>
 __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len, bool wide, int64_t r0) {
     constexpr int E = kVec<T>;
     constexpr int NB = (HBSJD_ADJUST_MAX_BIASES + NT - 1) / NT;
@@ -67,7 +75,8 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
     const int first = (blockIdx.x - row * parts) * len, V = min(len, a.V - first);
     const T* z = (const T*)a.logits + r * a.ld + first;
     O* o = (O*)a.out + r * a.ld_out + first;
-    const bool counts = a.tokens != nullptr, biases = a.n_bias > 0;
+    const bool counts = a.tokens != nullptr, listed = counts || Biased;
+    const uint32_t tag = wide ? 0x80000000u : 0x8000u;
 
     const Span sp = Span::of(z, V);
     const u32x4* z4 = (const u32x4*)(z + sp.head);
@@ -80,9 +89,10 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
 
     AdjustLds l;
     l.count = lds;
-    l.biased = l.count + (counts ? (count_words(len, wide) + 3) / 4 * 4 : 0);
-    l.mask = l.biased + (biases ? (len + 31) / 32 : 0);
+    l.biased = l.count + (listed ? (count_words(len, wide) + 3) / 4 * 4 : 0);
+    l.mask = l.biased + (Biased ? (len + 31) / 32 : 0);
     l.list = (int32_t*)(l.mask + (a.mask ? len / 32 + 2 : 0));
+    l.result = (float*)(l.list + a.n_bias);
 
     const uint32_t* mask = a.mask;
     bool bad = false;
@@ -94,9 +104,9 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
         if (mask)
             for (int i = t; i < len / 32 + 2; i += NT) l.mask[i] = mask[min((first >> 5) + i, words - 1)];
     }
-    if (counts)
+    if (listed)
         for (int i = t; i < count_words(V, wide); i += NT) l.count[i] = 0;
-    if (biases)
+    if (Biased)
         for (int i = t; i < (V + 31) / 32; i += NT) l.biased[i] = 0;
     if (t == 0) twice = 0;
     __syncthreads();
@@ -105,56 +115,72 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
         pen.theta = a.repetition ? a.repetition[r] : 1.f;
         pen.presence = a.presence ? a.presence[r] : 0.f;
         pen.frequency = a.frequency ? a.frequency[r] : 0.f;
-        const int held = a.token_count ? min(a.token_count[r], a.n_tokens) : a.n_tokens;
+        const unsigned held = a.token_count ? max(0, min(a.token_count[r], a.n_tokens)) : a.n_tokens;
         const int32_t* tok = a.tokens + r * a.ld_tokens;
-        for (int i = t; i < held; i += NT) {
-            const int64_t v = (int64_t)tok[i] - first;
-            if (v < 0 || v >= V) continue;
-            const int p = sp.place((int)v, V);
-            if (wide) atomicAdd(&l.count[p], 1u);
-            else atomicAdd(&l.count[p >> 1], 1u << (p & 1) * 16);
+        // two loads in flight a thread: 64 rows of 128257 with 4096 tokens take 16.4
+        // us so, 17.3 with one; more slow ordinary lists down
+        for (unsigned i = t; i < held; i += 2 * NT) {
+            int v[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) v[n] = tok[min(i + NT * n, held - 1)];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                if (i + NT * n >= held || v[n] < first || v[n] - first >= V) continue;
+                const int p = sp.place(v[n] - first, V);
+                if (wide) atomicAdd(&l.count[p], 1u);
+                else atomicAdd(&l.count[p >> 1], 1u << (p & 1) * 16);
+            }
         }
     }
-    // this thread's biased entries (-1: none, or not the first mention), their
-    // logits, gathered before anything is stored, and biases
+    // this thread's biased entries (-1: none), their logits and biases
     int bv[NB];
     float bz[NB], bb[NB];
-    if (biases) {
+    const float* bval = Biased ? a.bias_value + r * a.ld_bias : nullptr;
+    if constexpr (Biased) {
         const int32_t* bi = a.bias_index + r * a.ld_bias;
-        const float* bval = a.bias_value + r * a.ld_bias;
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const int i = t + NT * n;
             bv[n] = -1;
             if (i >= a.n_bias) continue;
-            const int64_t v = (int64_t)bi[i] - first;
-            const bool here = v >= 0 && v < V;
-            l.list[i] = here ? (int)v : -1;
+            const bool here = bi[i] >= first && bi[i] - first < V;
+            l.list[i] = here ? bi[i] - first : -1;
             if (!here) continue;
-            bv[n] = (int)v;
+            const int v = l.list[i];
+            bv[n] = v;
             bz[n] = widen(z[v]);
             bb[n] = bval[i];
             if (atomicOr(&l.biased[v >> 5], 1u << (v & 31)) >> (v & 31) & 1) twice = 1;
         }
     }
     __syncthreads();
-    if (biases && twice) {
-        // an entry listed more than once: its first mention adds them all, in order
-        const float* bval = a.bias_value + r * a.ld_bias;
+    auto count_of = [&](int p) -> uint32_t {
+        return !listed ? 0 : wide ? l.count[p] : l.count[p >> 1] >> (p & 1) * 16 & 0xFFFFu;
+    };
+    if constexpr (Biased) {
+        const bool searched = twice;
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            if (bv[n] < 0) continue;
             const int i = t + NT * n, v = bv[n];
-            bool mentioned = false;
-            for (int j = 0; j < i; ++j) mentioned |= l.list[j] == v;
-            if (mentioned) bv[n] = -1;
-            else
+            if (v < 0) continue;
+            if (searched) {
+                // an entry listed more than once: its first mention adds them all, in order
+                bool mentioned = false;
+                for (int j = 0; j < i; ++j) mentioned |= l.list[j] == v;
+                if (mentioned) continue;
                 for (int j = i + 1; j < a.n_bias; ++j)
                     if (l.list[j] == v) bb[n] = bb[n] + bval[j];
+            }
+            const int p = sp.place(v, V);
+            l.result[i] = pen(bz[n], count_of(p)) + bb[n];
+            if (wide) l.count[p] = tag | i;
+            else ((uint16_t*)l.count)[p] = (uint16_t)(tag | i);
         }
+        __syncthreads();
     }
-    auto count_of = [&](int p) -> uint32_t {
-        return !counts ? 0 : wide ? l.count[p] : l.count[p >> 1] >> (p & 1) * 16 & 0xFFFFu;
+    auto apply = [&](float x, uint32_t c) {
+        if constexpr (!Biased) return pen(x, c);
+        return c & tag ? l.result[c & (HBSJD_ADJUST_MAX_BIASES - 1)] : pen(x, c);
     };
     // the mask's bits from entry v of the part on
     auto allowed = [&](int v) -> uint32_t {
@@ -169,7 +195,7 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
         float y[E];
 #pragma unroll
         for (int q = 0; q < E; ++q) y[q] = vec_get<T>(x[i], q);
-        if (counts) {
+        if (listed) {
             uint32_t c[E];
             if (wide) {
 #pragma unroll
@@ -193,7 +219,7 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
             for (int q = 0; q < E; ++q) any |= c[q];
             if (any) {
 #pragma unroll
-                for (int q = 0; q < E; ++q) y[q] = pen(y[q], c[q]);
+                for (int q = 0; q < E; ++q) y[q] = apply(y[q], c[q]);
             }
         }
         if (mask) {
@@ -209,20 +235,9 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
     }
     if (t < sp.edges()) {
         const int v = sp.edge(t, V);
-        float y = pen(xe, count_of(sp.vecs * E + t));
+        float y = apply(xe, count_of(sp.vecs * E + t));
         if (mask && !(allowed(v) & 1)) y = -INFINITY;
         o[v] = narrow<O>(bad ? __builtin_nanf("") : y);
-    }
-    if (!biases || bad) return;
-    __syncthreads();   // the part's stores come first
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        const int v = bv[n];
-        if (v < 0) continue;
-        float y = pen(bz[n], count_of(sp.place(v, V)));
-        y = y + bb[n];
-        if (mask && !(allowed(v) & 1)) y = -INFINITY;
-        o[v] = narrow<O>(y);
     }
 }
 
@@ -232,16 +247,21 @@ template <typename T, typename O, int NT, int NV> void run(const AdjustArgs& a, 
     int parts = (a.V + most - 1) / most;
     const int len = ((a.V + parts - 1) / parts + 15) / 16 * 16;
     parts = (a.V + len - 1) / len;
-    const bool wide = a.n_tokens > 65535;
+    const bool wide = a.n_tokens > kCountMost;
     size_t lds = 0;
-    if (a.tokens) lds += (count_words(len, wide) + 3) / 4 * 4;
-    if (a.n_bias) lds += (len + 31) / 32 + a.n_bias;
+    if (a.tokens || a.n_bias) lds += (count_words(len, wide) + 3) / 4 * 4;
+    if (a.n_bias) lds += (len + 31) / 32 + 2 * a.n_bias;
     if (a.mask) lds += len / 32 + 2;
     lds = resident_lds(lds * 4, len * sizeof(T));
     by_slabs(
         a.rows,
         [&](int64_t r0, dim3 grid) {
-            hipLaunchKernelGGL((k_adjust<T, O, NT, NV>), grid, dim3(NT), lds, s, a, parts, len, wide, r0);
+            if (a.n_bias)
+                hipLaunchKernelGGL((k_adjust<T, O, NT, NV, true>), grid, dim3(NT), lds, s, a, parts, len,
+                                   wide, r0);
+            else
+                hipLaunchKernelGGL((k_adjust<T, O, NT, NV, false>), grid, dim3(NT), lds, s, a, parts, len,
+                                   wide, r0);
         },
         parts);
 }
@@ -251,7 +271,7 @@ template <typename T, typename O> void go(const AdjustArgs& a, hipStream_t s) {
     // rows over more CUs. 32-bit counts of the largest would not fit.
     const int vecs = a.V / kVec<T>;
     if (vecs <= 64 * 2) run<T, O, 64, 2>(a, s);
-    else if (a.rows * ((a.V + 16383) / 16384) < 512 || vecs <= 256 * 4 || a.n_tokens > 65535)
+    else if (a.rows * ((a.V + 16383) / 16384) < 512 || vecs <= 256 * 4 || a.n_tokens > kCountMost)
         run<T, O, 256, 4>(a, s);
     else run<T, O, 512, 16384 / kVec<T> / 512>(a, s);
 }

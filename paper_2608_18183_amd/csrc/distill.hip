@@ -372,6 +372,12 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     const float rest = a.rest ? a.rest[r] : -INFINITY;
     float* zk = p.zk + (int64_t)row * a.K;
     float* stats = p.stats + (int64_t)row * p.parts * 3;
+    float part_m = -INFINITY, part_s = 0.f, part_bad = 0.f;
+    if (Second && (t & 63) < p.parts) {
+        part_m = stats[3 * (t & 63)];
+        part_s = stats[3 * (t & 63) + 1];
+        part_bad = stats[3 * (t & 63) + 2];
+    }
     for (int i = t; i < (V + 31) / 32; i += NT) e.listed[i] = 0;
     if (t == 0) bad = 0;
     __syncthreads();
@@ -388,18 +394,13 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
             stats[3 * c + 2] = bad;
         }
     } else {
-        bool refused = uniform(bad) != 0;
-        float m0 = -INFINITY, s0 = 0.f;
-        for (int i = 0; i < p.parts; ++i) {
-            m0 = fmaxf(m0, stats[3 * i]);
-            refused |= stats[3 * i + 2] != 0.f;
-        }
+        // every wavefront joins the parts, a lane each
         block_all<NT, 2>(*(float(*)[2])(mm + 1), red, MaxOp());
+        float m0 = wave_all(part_m, MaxOp());
+        const bool refused = uniform(bad) || wave_all(part_bad, MaxOp()) > 0.f;
         if (m0 == -INFINITY) m0 = mm[1];
-        for (int i = 0; i < p.parts; ++i) {
-            const float m = stats[3 * i], s = stats[3 * i + 1];
-            s0 += m == -INFINITY ? s : s * power(m - m0, c2);
-        }
+        const float s0 =
+            wave_all(part_m == -INFINITY ? part_s : part_s * power(part_m - m0, c2), AddOp());
         const RowStats st = classes<NT>(a, e, rest, m0, mm[1], mm[2], t == 0 ? s0 : 0.f, refused, red + 3,
                                         red2, shared);
         if (a.loss && c == 0 && t == 0) a.loss[r] = w * st.loss;
@@ -435,7 +436,7 @@ Plan plan_of(int64_t rows, int V, int K, int32_t elem) {
     const int64_t held = 1024 * (elem == HBSJD_ELEM_F32 ? 8 : 16) * (16 / size);
     if (V <= kPart || (V <= held && rows >= 256)) return p;
     p.parts = (V + kPart - 1) / kPart;
-    while (rows * p.parts < 512 && V / (2 * p.parts) >= 4096) p.parts *= 2;
+    while (rows * p.parts < 512 && V / (2 * p.parts) >= 4096) p.parts *= 2;   // 64 at most: a lane each
     p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (V + p.len - 1) / p.len;
     // a slab's logits and gradient together stay within the last-level cache

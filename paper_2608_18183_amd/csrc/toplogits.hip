@@ -86,6 +86,9 @@ template <> struct Candidate<F16> : Candidate16<F16> {};
 
 // room for candidates
 constexpr int kFew = 1024, kMany = 4096;
+#ifndef PARTS_MIN
+#define PARTS_MIN 256
+#endif
 
 // Where a row's entries come from and its results go: a row of logits, or the
 // lists of a row's parts, whose entry v stands for entry map[v] and to whose
@@ -102,18 +105,18 @@ struct TopRow {
         values[k] = x;
         index[k] = map ? map[v] : first + v;
     }
-    // rest from the log of what the kernel itself left over
-    __device__ __forceinline__ void put_rest(float own) const {
-        float m = own;
-        for (int i = 0; i < n_rests; ++i) m = fmaxf(m, rests[i]);
-        if (n_rests && own == own && fabsf(m) != INFINITY) {
-            float s = __expf(own - m);
-            for (int i = 0; i < n_rests; ++i) s += __expf(rests[i] - m);
-            own = m + __logf(s);
-        } else if (n_rests && own == own) {
-            own = m;
+    // the rest of this lane's part (of 64 at most)
+    __device__ __forceinline__ float part_rest() const {
+        return (int)(threadIdx.x & 63) < n_rests ? rests[threadIdx.x & 63] : -INFINITY;
+    }
+    // rest from the log of what the kernel itself left over; by whole wavefronts
+    __device__ __forceinline__ void put_rest(float own, float part) const {
+        if (n_rests && own == own) {
+            const float m = fmaxf(own, wave_all(part, MaxOp()));
+            if (fabsf(m) == INFINITY) own = m;
+            else own = m + __logf(__expf(own - m) + wave_all(__expf(part - m), AddOp()));
         }
-        *rest = own;
+        if (threadIdx.x == 0) *rest = own;
     }
 };
 
@@ -177,9 +180,10 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
         }
     __syncthreads();
     for (int k = t; k < K; k += NT) out.put(k, logit_of(kept[k]), index_of(kept[k]));
-    if (t == 0) {
+    if (t < 64) {
         const bool nan = kept[0] >> 32 == 0xFFFFFFFFu;
-        out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s));
+        out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s),
+                     out.part_rest());
     }
 }
 
@@ -234,6 +238,8 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (t + NT * i >= sp.vecs) x[i] = masked_vec<T>();
+
+    const float part_rest = out.part_rest();
 
     // ---- 1. the pivot
     float p0 = -INFINITY;
@@ -499,11 +505,11 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         below = s;
         over = 0.f;
     }
-    if (t == 0) {
+    if (t < 64) {
         const float a = below > 0.f ? ref_below * inv_tau + __logf(below) : -INFINITY;
         const float b = over > 0.f ? ref_over * inv_tau + __logf(over) : -INFINITY;
         const float m = fmaxf(a, b);
-        out.put_rest(m == -INFINITY ? m : m + __logf(__expf(a - m) + __expf(b - m)));
+        out.put_rest(m == -INFINITY ? m : m + __logf(__expf(a - m) + __expf(b - m)), part_rest);
     }
 }
 
@@ -556,7 +562,7 @@ Plan plan_of(int64_t rows, int V, int K) {
     Plan p;
     if (V <= kPart) return p;
     p.parts = (V + kPart - 1) / kPart;
-    while (rows * p.parts < 256 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
+    while (rows * p.parts < PARTS_MIN && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
         p.parts *= 2;
     p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (V + p.len - 1) / p.len;

@@ -469,6 +469,23 @@ def test_adjust_shared_lists_nan_and_masks_that_leave_nothing():
     assert np.array_equal(own, np.where(allowed, x[:3], -np.inf), equal_nan=True)
 
 
+def test_adjust_ignores_entries_and_counts_out_of_range():
+    rng = np.random.default_rng(4)
+    big = 2 ** 31 - 1
+    x = rng.normal(0, 1, (4, 300)).astype(np.float32)
+    tok = rng.integers(0, 300, (4, 9)).astype(np.int32)
+    tok[:, ::2] = [-big - 1, -1, 300, 17, big]
+    count = np.array([9, -3, big, 0], np.int32)       # clamped to [0, 9]
+    bi = np.tile(np.array([-big - 1, 17, -1, 300, big, 17], np.int32), (4, 1))
+    bv = rng.normal(0, 1, (4, 6)).astype(np.float32)
+    freq = np.full(4, 0.5, np.float32)
+    got = P().hbsjd_adjust_rows(dev(x), tokens=dev(tok), token_count=dev(count), frequency=dev(freq),
+                                bias_index=dev(bi), bias_value=dev(bv)).cpu().numpy()
+    for r, n in enumerate((9, 0, 9, 0)):
+        assert np.array_equal(got[r], ref.adjust(x[r], tokens=tok[r, :n], frequency=0.5,
+                                                 bias=list(zip(bi[r], bv[r]))))
+
+
 def test_adjust_of_nothing_is_a_copy():
     x = torch.randn(9, 501, device="cuda").to(torch.bfloat16)
     assert torch.equal(P().hbsjd_adjust_rows(x), x)
