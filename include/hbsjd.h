@@ -279,7 +279,7 @@ hbsjd_status hbsjd_bikl_rows(const float* logits_s, const float* logits_t, int64
  * anything. All pointers are device memory of the current device.
  *
  * Calls on long rows need a workspace of the caller's, device memory (aligned to
- * 4 bytes) that a call uses until its kernels have run and whose contents mean
+ * 16 bytes) that a call uses until its kernels have run and whose contents mean
  * nothing before or after; hbsjd_top_logits_workspace and
  * hbsjd_distill_top_workspace say how many bytes (0 up to V = 16384 and for
  * arguments that would be refused). EINVAL when it is smaller. Calls that may

@@ -30,7 +30,7 @@ const char* rows_problem(int64_t rows, int32_t V) {
 
 const char* workspace_problem(const void* p, uint64_t bytes, uint64_t need) {
     if (need && (!p || bytes < need)) return "workspace smaller than the call needs";
-    if (need && !aligned(p, 4)) return "workspace not aligned to 4 bytes";
+    if (need && !aligned(p, 16)) return "workspace not aligned to 16 bytes";
     return nullptr;
 }
 

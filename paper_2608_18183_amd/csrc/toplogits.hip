@@ -86,13 +86,10 @@ template <> struct Candidate<F16> : Candidate16<F16> {};
 
 // room for candidates
 constexpr int kFew = 1024, kMany = 4096;
-#ifndef PARTS_MIN
-#define PARTS_MIN 256
-#endif
 
-// Where a row's entries come from and its results go: a row of logits, or the
-// lists of a row's parts, whose entry v stands for entry map[v] and to whose
-// rest the parts' rests are added.
+// Where a row's results go. A row of logits is a whole one or a part; a join's
+// row are the lists of a row's parts, whose place v holds entry map[v], and to
+// whose rest the parts' rests are added.
 struct TopRow {
     float* values;
     int32_t* index;
@@ -101,9 +98,25 @@ struct TopRow {
     const float* rests;
     int n_rests;
     int first;   // of the row's entries in the whole row
-    __device__ __forceinline__ void put(int k, float x, int v) const {
-        values[k] = x;
-        index[k] = map ? map[v] : first + v;
+    int parts;   // of a part: the row's; 0 otherwise
+    // how place v is to be called: its entry, for equal logits to be ordered by
+    __device__ __forceinline__ int entry(int v) const { return map ? map[v] : v; }
+    __device__ __forceinline__ void put(int k, float x, int entry, int K) const {
+        const int at = parts ? list_place(k, K, parts) : k;
+        values[at] = x;
+        index[at] = first + entry;
+    }
+    // What a part writes for a join. Four places in a row, one of the join's
+    // vectors, take the entries of one list a quarter of it apart: then the
+    // largest of each, by which the join finds its pivot, are the lists' first
+    // quarters, and the row's largest entries are mostly among those.
+    __device__ __forceinline__ static int list_place(int k, int K, int parts) {
+        const int q = (K + 3) / 4;
+        return (k % q * parts) * 4 + k / q;
+    }
+    __device__ __forceinline__ void pad(int K) const {
+        const int k = K + threadIdx.x;
+        if (parts && k < (K + 3) / 4 * 4) put(k, -INFINITY, 0x7FFFFFFF - first, K);
     }
     // the rest of this lane's part (of 64 at most)
     __device__ __forceinline__ float part_rest() const {
@@ -132,7 +145,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
         for (int i = t; i < 256; i += NT) hist[i] = 0;
         __syncthreads();
         for (int v = t; v < V; v += NT) {
-            const uint64_t c = ranked(widen(z[v]), v);
+            const uint64_t c = ranked(widen(z[v]), out.entry(v));
             if (shift == 56 || c >> (shift + 8) == prefix) atomicAdd(&hist[c >> shift & 255], 1);
         }
         __syncthreads();
@@ -151,7 +164,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
     float m = -INFINITY;
     for (int v = t; v < V; v += NT) {
         const float x = widen(z[v]);
-        const uint64_t c = ranked(x, v);
+        const uint64_t c = ranked(x, out.entry(v));
         if (c >= prefix) kept[atomicAdd(&word[2], 1)] = c;
         else m = fmaxf(m, x);
     }
@@ -162,7 +175,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
     float s = 0.f;
     for (int v = t; v < V; v += NT) {
         const float x = widen(z[v]);
-        if (ranked(x, v) < prefix) s += __expf((x - m) * inv_tau);
+        if (ranked(x, out.entry(v)) < prefix) s += __expf((x - m) * inv_tau);
     }
     __syncthreads();
     s = block_all<NT>(s, red, AddOp());
@@ -179,7 +192,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
             }
         }
     __syncthreads();
-    for (int k = t; k < K; k += NT) out.put(k, logit_of(kept[k]), index_of(kept[k]));
+    for (int k = t; k < K; k += NT) out.put(k, logit_of(kept[k]), index_of(kept[k]), K);
     if (t < 64) {
         const bool nan = kept[0] >> 32 == 0xFFFFFFFFu;
         out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s),
@@ -208,7 +221,7 @@ template <int NV> __device__ __forceinline__ void opaque(u32x4 (&x)[NV]) {
     for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
 }
 
-template <typename T, int NT, int NV, int Cap>
+template <typename T, int NT, int NV, int Cap, bool Join>
 __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out) {
     constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
     static_assert(N >= 8, "eight groups a thread");
@@ -227,17 +240,21 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
     const float c2 = inv_tau * kLog2e;
 
+    // The thread's first vector. A join's vectors are nearly in order: they are
+    // dealt out one by one, so that every wavefront has its share of the largest.
+    const int t0 = Join ? lane * NW + wv : t;
     const Span sp = Span::of(z, V);
     const u32x4* z4 = (const u32x4*)(z + sp.head);
     u32x4 x[NV];
     float xe = -INFINITY;
     if (sp.vecs > 0)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min(t + NT * i, sp.vecs - 1));
+        for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min(t0 + NT * i, sp.vecs - 1));
     if (t < sp.edges()) xe = widen(z[sp.edge(t, V)]);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (t + NT * i >= sp.vecs) x[i] = masked_vec<T>();
+        if (t0 + NT * i >= sp.vecs) x[i] = masked_vec<T>();
+    out.pad(K);
 
     const float part_rest = out.part_rest();
 
@@ -256,7 +273,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         int groups = 8;
 #pragma unroll
         for (int h = 4; h > 0; h /= 2)
-            if (groups == 2 * h && NT * h >= 2 * K) {
+            if (!Join && groups == 2 * h && NT * h >= 2 * K) {
 #pragma unroll
                 for (int b = 0; b < h; ++b) g[b] = fmaxf(g[b], g[b + h]);
                 groups = h;
@@ -343,10 +360,10 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 #pragma unroll
         for (int q = 0; q < E; ++q) {
             const float y = vec_get<T>(x[i], q);
-            if (y >= from) cand[slot++] = Cand::of(y, sp.head + (t + NT * i) * E + q);
+            if (y >= from) cand[slot++] = Cand::of(y, out.entry(sp.head + (t0 + NT * i) * E + q));
         }
     }
-    if (xe >= from) cand[slot++] = Cand::of(xe, sp.edge(t, V));
+    if (xe >= from) cand[slot++] = Cand::of(xe, out.entry(sp.edge(t, V)));
 
     // ---- 3. places
     constexpr int M = Cap / NT;   // candidates a thread looks after
@@ -374,7 +391,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
                     for (int q = 0; q < 16 / (int)sizeof(Key); ++q) p += other[q] > me[n];
                 }
             place[n] = p;
-            if (p < K) out.put(p, Cand::logit(me[n]), Cand::index(me[n]));
+            if (p < K) out.put(p, Cand::logit(me[n]), Cand::index(me[n]), K);
             if (p == K - 1) s_last = Cand::logit(me[n]);
         }
         __syncthreads();
@@ -464,7 +481,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         for (int n = 0; n < M; ++n)
             if (place[n] < K) cand[place[n]] = me[n];
         __syncthreads();
-        for (int k = t; k < K; k += NT) out.put(k, Cand::logit(cand[k]), Cand::index(cand[k]));
+        for (int k = t; k < K; k += NT) out.put(k, Cand::logit(cand[k]), Cand::index(cand[k]), K);
     }
 
     // ---- the mass of the others: below the pivot, and the candidates left over
@@ -516,37 +533,36 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
 template <typename T, int NT, int NV, int Cap>
 __global__ __launch_bounds__(NT) void k_top(TopArgs a, int64_t r0) {
     const int64_t r = r0 + blockIdx.x;
-    const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0};
-    top_row<T, NT, NV, Cap>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out);
+    const TopRow out{a.values + r * a.K, a.index + r * a.K, a.rest + r, nullptr, nullptr, 0, 0, 0};
+    top_row<T, NT, NV, Cap, false>((const T*)a.logits + r * a.ld, a.V, a.K, a.inv_tau, out);
 }
 
 // Long rows: every part's K largest and the mass of its others go to the
-// workspace, and the row's are the K largest of the parts'. Lists are in
-// descending order with the lowest index first and parts follow one another, so
-// equal logits keep the order of their entries.
+// workspace, and the row's are the K largest of the parts'.
 struct PartsArgs {
     int parts, len;
-    float* values;   // [rows of the slab][parts][K]
+    float* values;   // [rows of the slab][list_room(K) * parts]
     int32_t* index;
     float* rest;     // [rows of the slab][parts]
 };
+__host__ __device__ inline int list_room(int K) { return (K + 3) / 4 * 4; }
 
 template <typename T, int NT, int NV, int Cap>
 __global__ __launch_bounds__(NT) void k_top_part(TopArgs a, PartsArgs p, int64_t r0) {
     const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
     const int first = c * p.len;
-    const int64_t at = blockIdx.x;
-    const TopRow out{p.values + at * a.K, p.index + at * a.K, p.rest + at, nullptr, nullptr, 0, first};
-    top_row<T, NT, NV, Cap>((const T*)a.logits + (r0 + row) * a.ld + first, min(p.len, a.V - first), a.K,
-                            a.inv_tau, out);
+    const int64_t at = (int64_t)row * list_room(a.K) * p.parts + 4 * c;
+    const TopRow out{p.values + at, p.index + at, p.rest + blockIdx.x, nullptr, nullptr, 0, first, p.parts};
+    top_row<T, NT, NV, Cap, false>((const T*)a.logits + (r0 + row) * a.ld + first,
+                                   min(p.len, a.V - first), a.K, a.inv_tau, out);
 }
 
 template <int NT, int NV, int Cap>
 __global__ __launch_bounds__(NT) void k_top_join(TopArgs a, PartsArgs p, int64_t r0) {
-    const int64_t row = blockIdx.x, r = r0 + row, n = (int64_t)p.parts * a.K;
-    const TopRow out{a.values + r * a.K,  a.index + r * a.K, a.rest + r, p.index + row * n,
-                     p.rest + row * p.parts, p.parts,           0};
-    top_row<float, NT, NV, Cap>(p.values + row * n, (int)n, a.K, a.inv_tau, out);
+    const int64_t row = blockIdx.x, r = r0 + row, n = (int64_t)list_room(a.K) * p.parts;
+    const TopRow out{a.values + r * a.K,     a.index + r * a.K, a.rest + r, p.index + row * n,
+                     p.rest + row * p.parts, p.parts,           0,          0};
+    top_row<float, NT, NV, Cap, true>(p.values + row * n, (int)n, a.K, a.inv_tau, out);
 }
 
 // How a call runs: whole rows, or in parts with workspace for `slab` rows.
@@ -554,7 +570,7 @@ struct Plan {
     int parts = 0, len = 0;
     int64_t slab = 0;
 };
-inline size_t part_row_bytes(const Plan& p, int K) { return (size_t)p.parts * (8 * (size_t)K + 4); }
+inline size_t part_row_bytes(const Plan& p, int K) { return (size_t)p.parts * (8 * (size_t)list_room(K) + 4); }
 
 // Rows of more entries than a workgroup holds go in parts; where rows are few,
 // in more and smaller ones, as long as the join stays the smaller work.
@@ -562,7 +578,7 @@ Plan plan_of(int64_t rows, int V, int K) {
     Plan p;
     if (V <= kPart) return p;
     p.parts = (V + kPart - 1) / kPart;
-    while (rows * p.parts < PARTS_MIN && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
+    while (rows * p.parts < 256 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
         p.parts *= 2;
     p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (V + p.len - 1) / p.len;
@@ -610,8 +626,9 @@ template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
         return;
     }
     PartsArgs p{plan.parts, plan.len, (float*)ws, nullptr, nullptr};
-    p.index = (int32_t*)(p.values + plan.slab * plan.parts * a.K);
-    p.rest = (float*)(p.index + plan.slab * plan.parts * a.K);
+    const int64_t lists = plan.slab * plan.parts * list_room(a.K);
+    p.index = (int32_t*)(p.values + lists);
+    p.rest = (float*)(p.index + lists);
     for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
         const int64_t n = std::min(plan.slab, a.rows - r0);
         by_size<T>(p.len, a.K, 256, [&](auto nt, auto nv, auto cap) {
@@ -620,7 +637,7 @@ template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
                 hipLaunchKernelGGL((k_top_part<T, NT, NV, Cap>), dim3((unsigned)(n * p.parts)), dim3(NT),
                                    0, s, a, p, r0);
         });
-        by_size<float>(p.parts * a.K, a.K, 256, [&](auto nt, auto nv, auto cap) {
+        by_size<float>(p.parts * list_room(a.K), a.K, 256, [&](auto nt, auto nv, auto cap) {
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
             if constexpr (NT >= 256)
                 hipLaunchKernelGGL((k_top_join<NT, NV, Cap>), dim3((unsigned)n), dim3(NT), 0, s, a, p, r0);

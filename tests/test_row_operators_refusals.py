@@ -80,7 +80,7 @@ def test_long_rows_need_their_workspace():
         long = dict(V=200000, ld=200000, **({"ld_grad": 200000} if call is _distill else {}))
         assert call(**long) == "EINVAL"
         assert call(workspace=A, workspace_bytes=need - 1, **long) == "EINVAL"
-        assert call(workspace=A + 2, workspace_bytes=need, **long) == "EINVAL"
+        assert call(workspace=A + 8, workspace_bytes=need, **long) == "EINVAL"
         for bad in ((0, 200000, 0, 5), (5, 300000, 0, 5), (5, 200000, 4, 5), (5, 200000, 0, 0),
                     (5, 200000, 0, 4000)):
             assert f(*bad) == 0
