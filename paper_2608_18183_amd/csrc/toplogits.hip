@@ -16,7 +16,7 @@
 //      over all of them when they are few, else over those of its bin, in bins
 //      of equal width between the least and the largest candidate.
 // Rows on which this fails (more candidates or equal ones than there is room
-// for, fewer than K entries above -infinity, NaN) take digit-by-digit selection
+// for, fewer than K entries above -infinity, NaN, a pivot next to fp32's ends) take digit-by-digit selection
 // and a bitonic sort instead, with the same results.
 #include "rows.h"
 
@@ -280,12 +280,14 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
             }
         const int want = (K + NW - 1) / NW;
         uint32_t pivot = 0;
-        // the upper 24 bits will do: a lower pivot is a pivot too
+        // the upper 24 bits will do (a lower pivot is a pivot too), or all that the
+        // images of 16-bit logits have
+        constexpr int kLowest = std::is_same_v<T, Bf16> ? 16 : std::is_same_v<T, F16> ? 13 : 8;
         auto descend = [&](auto n) {
             uint32_t key[decltype(n)::value];
 #pragma unroll
             for (int b = 0; b < decltype(n)::value; ++b) key[b] = order_of(g[b]);
-            for (int bit = 31; bit >= 8; --bit) {
+            for (int bit = 31; bit >= kLowest; --bit) {
                 const uint32_t next = pivot | 1u << bit;
                 int have = 0;
 #pragma unroll
@@ -308,7 +310,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     }
     // -infinity is nobody's candidate
     const float from = fmaxf(p0, -3.4028234663852886e38f);
-    const float ref = p0 == -INFINITY ? 0.f : p0;
+    const float ref = p0 == -INFINITY ? 0.f : p0, ref2 = -ref * c2;
 
     // ---- 2. candidates, and the mass below them
     opaque(x);
@@ -320,7 +322,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         for (int q = 0; q < E; ++q) {
             const float y = vec_get<T>(x[i], q);
             const bool in = y >= from;
-            const float e = __builtin_amdgcn_exp2f((y - ref) * c2);
+            const float e = __builtin_amdgcn_exp2f(fmaf(y, c2, ref2));
             mine += in;
             below += in ? 0.f : e;
         }
@@ -329,7 +331,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     {
         const bool in = xe >= from;
         mine += in;
-        below += in ? 0.f : __builtin_amdgcn_exp2f((xe - ref) * c2);
+        below += in ? 0.f : __builtin_amdgcn_exp2f(fmaf(xe, c2, ref2));
     }
     int total;
     int slot = wave_prefix(mine, total);
@@ -349,7 +351,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     }
     C = uniform(C);
     below = uniform(below);
-    if (C > Cap || C < K || below != below) {
+    if (C > Cap || C < K || below != below || fabsf(ref2) == INFINITY) {
         __syncthreads();
         top_by_digits<NT>(z, V, K, inv_tau, out, (uint64_t*)room, bins, red[0], word);
         return;

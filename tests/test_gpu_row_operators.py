@@ -68,7 +68,11 @@ def check_top(x64, out, k, tau):
     assert np.array_equal(values.astype(np.float64), wv)
     n = x64.shape[1]
     for r in range(x64.shape[0]):
-        if np.isfinite(wr[r]):
+        if np.abs(wr[r]) > np.finfo(np.float32).max:
+            # rest is fp32: beyond 2^128 (1 - 2^-25) the nearest is an infinity, and
+            # the logits here lie well past that or well below it
+            assert rest[r] == np.sign(wr[r]) * np.inf
+        elif np.isfinite(wr[r]):
             s = wr[r] - np.where(np.isfinite(wv[r, -1]), wv[r, -1], 0) / tau
             left = np.delete(x64[r], wi[r]).max() / tau
             # m / tau (two roundings), the log of the sum, their sum
@@ -111,6 +115,23 @@ def test_top_logits_of_equal_and_ordered_rows(V):
     for k in sorted({1, 5, 64, min(V, 1000)}):
         got = P().hbsjd_top_logits_rows(dev(x), k, temperature=1.0)
         check_top(x.astype(np.float64), got, k, 1.0)
+
+
+@pytest.mark.parametrize("V", [300, 5000, 40000])
+def test_top_logits_far_from_zero(V):
+    """Masks left at several values next to fp32's lowest, with and without
+    -infinity among them, and rows that are all large."""
+    rng = np.random.default_rng(V)
+    x = rng.uniform(-3.39e38, -2e38, (5, V)).astype(np.float32)
+    x[0, ::V // 5] = rng.normal(0, 1, x[0, ::V // 5].size)
+    x[1, ::7] = -np.inf
+    x[2] = -x[2]
+    x[3] = rng.normal(0, 1, V) * 1e30
+    x[4] = rng.normal(0, 1, V) - 90.0
+    x[4, :20] += 200.0
+    for k in (1, 8, 50, 200):
+        for tau in (0.5, 1.0):
+            check_top(x.astype(np.float64), P().hbsjd_top_logits_rows(dev(x), k, temperature=tau), k, tau)
 
 
 def test_top_logits_of_rows_with_nan_and_infinity():
