@@ -25,6 +25,7 @@ PROGRESS_INDEPENDENT, PROGRESS_SYNC = 0, 1
 KERNELS = ["setup", "embed", "qkv", "attn", "oproj", "norm", "w13", "w2", "lmhead",
            "transform", "verify", "bikl"]
 _WHOLE_ROWS = 16384   # rows of more entries may need a workspace
+_INT_MAX = 2 ** 31 - 1   # ctypes would cut larger numbers off
 _STATUS = {0: "OK", 1: "EINVAL", 2: "ENOMEM", 3: "EHIP", 4: "ESTATE", 5: "EINTERNAL"}
 
 _P = ctypes.c_void_p
@@ -410,6 +411,8 @@ def _matrix(t, what: str, like=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what}: expected a device tensor [rows, V]")
     rows, V = t.shape
+    if V > _INT_MAX:
+        raise ValueError(f"{what}: rows of {V} entries")
     if like is not None and (t.shape != like.shape or t.device != like.device):
         raise ValueError(f"{what}: expected shape {tuple(like.shape)} on {like.device}")
     ld, step = t.stride()
@@ -442,6 +445,8 @@ def _lists(t, what: str, rows: int, dtype, device):
     if len(shape) not in (1, 2) or (len(shape) == 2 and shape[0] != rows):
         raise ValueError(f"{what}: expected shape [{rows}, n] or [n]")
     n = shape[-1]
+    if n > _INT_MAX:
+        raise ValueError(f"{what}: lists of {n} entries")
     if n > 1 and t.stride(-1) != 1:
         raise ValueError(f"{what}: the entries of a list have to be adjacent")
     return n, t.stride(0) if len(shape) == 2 and rows > 1 else 0
@@ -486,7 +491,7 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
     import torch
     rows, V, ld = _matrix(logits, "logits")
     elem, dev, k = _elem(logits.dtype), logits.device, int(k)
-    if k < 1:
+    if not 1 <= k <= _INT_MAX:
         raise ValueError("need k >= 1")
     L = load_library()
 
@@ -523,7 +528,7 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
     elem, dev = _elem(logits.dtype), logits.device
     if values is None or index is None or values.dim() != 2:
         raise ValueError(f"values and index: expected tensors of shape [{rows}, K]")
-    K = values.shape[1]
+    K = min(values.shape[1], _INT_MAX)
     f32 = torch.float32
     a = _DistillArgs(rows, V, K, logits.data_ptr(), ld, elem, temperature,
                      _vector(values, "values", (rows, K), f32, dev),
@@ -586,8 +591,8 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     if mask is not None:
         n_masks = mask.shape[0]
         at["mask"] = _vector(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
-        if n_masks == 0:
-            raise ValueError("mask: no masks")
+        if not 1 <= n_masks <= _INT_MAX:
+            raise ValueError(f"mask: {n_masks} masks")
     a = _AdjustArgs(rows, V, elem, logits.data_ptr(), ld, at["tokens"], n_tokens, ld_tokens,
                     _vector(token_count, "token_count", row, i32, dev),
                     _vector(repetition, "repetition", row, f32, dev),

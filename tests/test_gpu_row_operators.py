@@ -513,6 +513,60 @@ def test_adjust_of_nothing_is_a_copy():
     assert torch.equal(P().hbsjd_adjust_rows(x, out_dtype=torch.float32), x.float())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_rows_in_error_are_nan_in_every_type(dtype):
+    rng = np.random.default_rng(12)
+    n, V, k = 4, 301, 6
+    t, x64 = rows_of(rng, n, V, dtype)
+    values, index, rest = teacher_of(rng, x64, k, 1.0)
+    index[1, 2] = V + 5
+    loss, grad = P().hbsjd_distill_top_rows(t.cuda(), dev(values), dev(index), dev(rest))
+    keep = [0, 2, 3]
+    assert bool(torch.isnan(loss[1])) and bool(torch.isnan(grad[1]).all())
+    check_distill(x64[keep], values[keep], index[keep], rest[keep], np.ones(3), 1.0, 0.5, 0.5,
+                  loss[keep], grad[keep], dtype)
+    ok = dev(ref.pack_mask(np.ones((1, V), bool)))
+    which = dev(np.array([0, 1, -1, 0], np.int32))
+    for out_dtype in (TYPES[dtype], torch.float32):
+        y = P().hbsjd_adjust_rows(t.cuda(), mask=ok, mask_row=which, out_dtype=out_dtype)
+        assert bool(torch.isnan(y[1]).all())
+        assert torch.equal(y[keep], t.cuda()[keep].to(out_dtype))
+
+
+@pytest.mark.parametrize("V", [500, 20000])
+def test_offsets_past_32_bits(V):
+    """Rows 1.2e9 entries apart: the third starts past 2^31 entries and 2^32 bytes."""
+    rng = np.random.default_rng(13)
+    n, k, ld = 3, 9, 1_200_000_007
+    t, x64 = rows_of(rng, n, V, "bf16")
+    buf = torch.empty(2 * ld + V, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (n, V), (ld, 1))
+    x.copy_(t)
+    check_top(x64, P().hbsjd_top_logits_rows(x, k), k, 1.0)
+    values, index, rest = teacher_of(rng, x64, k, 1.0)
+    tok = rng.integers(0, V, (n, 50)).astype(np.int32)
+    freq = np.full(n, 0.5, np.float32)
+    y = P().hbsjd_adjust_rows(x, tokens=dev(tok), frequency=dev(freq), out_dtype=torch.float32)
+    for r in range(n):
+        assert np.array_equal(y[r].cpu().numpy(),
+                              ref.adjust(t[r].float().numpy(), tokens=tok[r], frequency=0.5))
+    loss, grad = P().hbsjd_distill_top_rows(x, dev(values), dev(index), dev(rest), grad=x)
+    check_distill(x64, values, index, rest, np.ones(n), 1.0, 0.5, 0.5, loss, grad.contiguous(), "bf16")
+
+
+def test_list_lengths_and_positions_of_every_kind_of_k():
+    """K at the sizes where the selection changes its workgroups, its room and its
+    way of placing, on random, tied and ordered rows."""
+    rng = np.random.default_rng(14)
+    for V in (1024, 1025, 4097, 16384, 50000):
+        for dtype in ("f32", "bf16"):
+            rows = [rng.normal(0, 2, V), np.round(rng.normal(0, 2, V)), np.sort(rng.normal(0, 2, V)),
+                    np.linspace(5, -5, V) + rng.normal(0, 0.5, V)]
+            t = torch.from_numpy(np.stack(rows).astype(np.float32)).to(TYPES[dtype])
+            for k in (31, 32, 33, 128, 129, 255, 256, 257, 511, 513, 1024):
+                check_top(t.double().numpy(), P().hbsjd_top_logits_rows(t.cuda(), k), k, 1.0)
+
+
 # ------------------------------------------------------------------ as calls
 
 def all_three(x, tok, freq, k, stream=None):
