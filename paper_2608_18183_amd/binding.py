@@ -392,23 +392,30 @@ def hbsjd_bikl_rows(logits_s, logits_t, stream=None):
 
 # The calls below take 5 us on the GPU where rows are few, so that the time of a
 # call is the host's: checks that pass cost one comparison each, pointers go to
-# ctypes as plain integers.
+# ctypes as plain integers, and torch is looked up once.
+
+_torch = None
+_ELEMS = {}
+
+
+def _load_torch():
+    global _torch
+    import torch
+    _ELEMS.update({torch.float32: ELEM_F32, torch.bfloat16: ELEM_BF16, torch.float16: ELEM_F16})
+    _torch = torch
+    return torch
+
 
 def _elem(dtype) -> int:
-    import torch
-    if dtype is torch.float32:
-        return ELEM_F32
-    if dtype is torch.bfloat16:
-        return ELEM_BF16
-    if dtype is torch.float16:
-        return ELEM_F16
-    raise ValueError(f"rows of logits are fp32, bf16 or fp16, not {dtype}")
+    try:
+        return _ELEMS[dtype]
+    except KeyError:
+        raise ValueError(f"rows of logits are fp32, bf16 or fp16, not {dtype}") from None
 
 
 def _matrix(t, what: str, like=None):
     """A device tensor [rows, V] whose rows are contiguous: (rows, V, row stride)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{what}: expected a device tensor [rows, V]")
     rows, V = t.shape
     if V > _INT_MAX:
@@ -416,7 +423,7 @@ def _matrix(t, what: str, like=None):
     if like is not None and (t.shape != like.shape or t.device != like.device):
         raise ValueError(f"{what}: expected shape {tuple(like.shape)} on {like.device}")
     ld, step = t.stride()
-    if V > 1 and step != 1:
+    if step != 1 and V > 1:
         raise ValueError(f"{what}: the entries of a row have to be adjacent")
     if rows <= 1:
         ld = V
@@ -429,7 +436,7 @@ def _vector(t, what: str, shape, dtype, device):
     """The address of a contiguous device tensor of this shape and type, or None."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype is not dtype:
+    if not isinstance(t, _torch.Tensor) or t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}")
     if t.device != device or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor on {device}")
@@ -438,8 +445,8 @@ def _vector(t, what: str, shape, dtype, device):
 
 def _lists(t, what: str, rows: int, dtype, device):
     """Lists of one length for every row, [rows, n], or [n] for all rows: their
-    length and row stride."""
-    if t.dtype is not dtype or t.device != device:
+    length, row stride and address."""
+    if not isinstance(t, _torch.Tensor) or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{what}: expected {dtype} on {device}")
     shape = t.shape
     if len(shape) not in (1, 2) or (len(shape) == 2 and shape[0] != rows):
@@ -449,38 +456,40 @@ def _lists(t, what: str, rows: int, dtype, device):
         raise ValueError(f"{what}: lists of {n} entries")
     if n > 1 and t.stride(-1) != 1:
         raise ValueError(f"{what}: the entries of a list have to be adjacent")
-    return n, t.stride(0) if len(shape) == 2 and rows > 1 else 0
+    return n, t.stride(0) if len(shape) == 2 and rows > 1 else 0, t.data_ptr()
 
 
-def _workspace(nbytes: int, device):
-    """Device memory for one call: allocated for the stream that the call runs on,
-    so that its next owner comes after the call's kernels."""
-    import torch
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+class _OnStream:
+    """Makes `device` and `stream` the current ones for a call that does not wait, so
+    that its outputs are allocated for that stream, and tells the caching allocator
+    that the stream uses `tensors`: the caller may drop them at once."""
+
+    def __init__(self, device, stream, tensors):
+        torch = _torch
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        elif not hasattr(stream, "cuda_stream"):
+            stream = (torch.cuda.ExternalStream(int(stream), device=device) if int(stream)
+                      else torch.cuda.default_stream(device))
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the logits on {device}")
+        self._stream, self._tensors = stream, tensors
+        self._context = torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self._context.__enter__()
+        return self._stream.cuda_stream
+
+    def __exit__(self, *exc):
+        for t in self._tensors:
+            if isinstance(t, _torch.Tensor):
+                t.record_stream(self._stream)
+        self._context.__exit__(*exc)
 
 
-def _on_stream(call, device, stream, tensors):
-    """call(handle) with the current device and stream being `device` and `stream`
-    (None: the device's current one), so that outputs are allocated for that
-    stream. The caching allocator is told that the stream uses `tensors`: the
-    calls do not wait, and the caller may drop them at once."""
-    import torch
-    if stream is None:
-        if device.index == torch.cuda.current_device():
-            return call(torch._C._cuda_getCurrentRawStream(device.index))
-        with torch.cuda.device(device):
-            return call(torch.cuda.current_stream().cuda_stream)
-    if not hasattr(stream, "cuda_stream"):
-        stream = (torch.cuda.ExternalStream(int(stream), device=device) if int(stream)
-                  else torch.cuda.default_stream(device))
-    if stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the logits on {device}")
-    with torch.cuda.stream(stream):
-        out = call(stream.cuda_stream)
-        for t in tensors:
-            if isinstance(t, torch.Tensor):
-                t.record_stream(stream)
-        return out
+def _here(device, stream) -> bool:
+    """Whether a call runs on the current device's current stream."""
+    return stream is None and device.index == _torch._C._cuda_getDevice()
 
 
 def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None, out=None):
@@ -488,31 +497,36 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
     Returns device tensors (values fp32 [rows, k], index int32 [rows, k], rest
     fp32 [rows]), written into `out` when given. Asynchronous on `stream` (the
     current one by default), as are the two calls below."""
-    import torch
+    torch = _torch or _load_torch()
     rows, V, ld = _matrix(logits, "logits")
-    elem, dev, k = _elem(logits.dtype), logits.device, int(k)
+    elem, dev = _elem(logits.dtype), logits.device
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, *(out or ()))):
+            return hbsjd_top_logits_rows(logits, k, temperature, None, out)
+    k = int(k)
     if not 1 <= k <= _INT_MAX:
         raise ValueError("need k >= 1")
-    L = load_library()
-
-    def call(handle):
-        if out is None:
-            values = logits.new_empty((rows, k), dtype=torch.float32)
-            index = logits.new_empty((rows, k), dtype=torch.int32)
-            rest = logits.new_empty((rows,), dtype=torch.float32)
-        else:
-            values, index, rest = out
-        nbytes = L.hbsjd_top_logits_workspace(rows, V, elem, k) if V > _WHOLE_ROWS else 0
-        ws = _workspace(nbytes, dev)
-        _check(L.hbsjd_top_logits_rows(
-            rows, V, logits.data_ptr(), elem, ld, k, temperature,
-            _vector(values, "values", (rows, k), torch.float32, dev),
-            _vector(index, "index", (rows, k), torch.int32, dev),
-            _vector(rest, "rest", (rows,), torch.float32, dev),
-            None if ws is None else ws.data_ptr(), nbytes, handle), "hbsjd_top_logits_rows")
-        return values, index, rest
-
-    return _on_stream(call, dev, stream, (logits, *(out or ())))
+    if out is None:
+        values = logits.new_empty((rows, k), dtype=torch.float32)
+        index = logits.new_empty((rows, k), dtype=torch.int32)
+        rest = logits.new_empty((rows,), dtype=torch.float32)
+        at = values.data_ptr(), index.data_ptr(), rest.data_ptr()
+    else:
+        values, index, rest = out
+        at = (_vector(values, "values", (rows, k), torch.float32, dev),
+              _vector(index, "index", (rows, k), torch.int32, dev),
+              _vector(rest, "rest", (rows,), torch.float32, dev))
+    L = _lib or load_library()
+    ws, nbytes = None, 0
+    if V > _WHOLE_ROWS:
+        nbytes = L.hbsjd_top_logits_workspace(rows, V, elem, k)
+        ws = logits.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+    st = L.hbsjd_top_logits_rows(rows, V, logits.data_ptr(), elem, ld, k, temperature, *at,
+                                 None if ws is None else ws.data_ptr(), nbytes,
+                                 torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_top_logits_rows")
+    return values, index, rest
 
 
 def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float = 1.0,
@@ -523,41 +537,45 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
     [rows] as hbsjd_top_logits_rows gives them for the teacher; row_weight fp32
     [rows]. Returns (loss fp32 [rows], grad like logits). grad=False leaves the
     gradient out (None), a tensor is written (the logits themselves too)."""
-    import torch
+    torch = _torch or _load_torch()
     rows, V, ld = _matrix(logits, "logits")
     elem, dev = _elem(logits.dtype), logits.device
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, values, index, rest, row_weight, grad)):
+            return hbsjd_distill_top_rows(logits, values, index, rest, temperature, forward_weight,
+                                          reverse_weight, row_weight, grad)
     if values is None or index is None or values.dim() != 2:
         raise ValueError(f"values and index: expected tensors of shape [{rows}, K]")
-    K = min(values.shape[1], _INT_MAX)
-    f32 = torch.float32
+    shape, row, f32 = values.shape, (rows,), torch.float32
+    K = min(shape[1], _INT_MAX)
     a = _DistillArgs(rows, V, K, logits.data_ptr(), ld, elem, temperature,
                      _vector(values, "values", (rows, K), f32, dev),
-                     _vector(index, "index", (rows, K), torch.int32, dev),
-                     _vector(rest, "rest", (rows,), f32, dev), forward_weight, reverse_weight,
-                     _vector(row_weight, "row_weight", (rows,), f32, dev))
-    L = load_library()
-
-    def call(handle):
-        loss = logits.new_empty((rows,), dtype=f32)
-        g = grad
-        if g is True:
-            g = logits.new_empty((rows, V))
-        ld_grad, address = 0, None
-        if g is False:
-            g = None
-        if g is not None:
-            ld_grad = _matrix(g, "grad", logits)[2]
-            if g.dtype is not logits.dtype:
-                raise ValueError("grad: expected the logits' type")
-            address = g.data_ptr()
-        nbytes = L.hbsjd_distill_top_workspace(rows, V, elem, K) if V > _WHOLE_ROWS else 0
-        ws = _workspace(nbytes, dev)
-        _check(L.hbsjd_distill_top_rows(ctypes.byref(a), loss.data_ptr(), address, ld_grad,
-                                        None if ws is None else ws.data_ptr(), nbytes, handle),
-               "hbsjd_distill_top_rows")
-        return loss, g
-
-    return _on_stream(call, dev, stream, (logits, values, index, rest, row_weight, grad))
+                     _vector(index, "index", shape, torch.int32, dev),
+                     _vector(rest, "rest", row, f32, dev), forward_weight, reverse_weight,
+                     _vector(row_weight, "row_weight", row, f32, dev))
+    loss = logits.new_empty(row, dtype=f32)
+    ld_grad, address = V, None
+    if grad is True:
+        grad = logits.new_empty((rows, V))
+        address = grad.data_ptr()
+    elif grad is False or grad is None:
+        grad = None
+    else:
+        ld_grad = _matrix(grad, "grad", logits)[2]
+        if grad.dtype is not logits.dtype:
+            raise ValueError("grad: expected the logits' type")
+        address = grad.data_ptr()
+    L = _lib or load_library()
+    ws, nbytes = None, 0
+    if V > _WHOLE_ROWS:
+        nbytes = L.hbsjd_distill_top_workspace(rows, V, elem, K)
+        ws = logits.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+    st = L.hbsjd_distill_top_rows(a, loss.data_ptr(), address, ld_grad,
+                                  None if ws is None else ws.data_ptr(), nbytes,
+                                  torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_distill_top_rows")
+    return loss, grad
 
 
 def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, presence=None,
@@ -569,55 +587,59 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     bias_value fp32 [rows, n] (or [n]); mask int32 [masks, ceil(V / 32)], a bit
     per allowed entry, with mask_row int32 [rows]. Returns the adjusted rows: a
     new tensor of out_dtype (the logits' type by default; fp32 is what
-    hbsjd_transform_rows takes), or `out`, which may be the logits."""
-    import torch
+    hbsjd_transform_rows takes), or `out`, which may be the logits. With nothing
+    to adjust, no `out` and the logits' type it returns the logits themselves, as
+    a tensor's to() does."""
+    torch = _torch or _load_torch()
     rows, V, ld = _matrix(logits, "logits")
-    elem, dev = _elem(logits.dtype), logits.device
+    dtype, dev = logits.dtype, logits.device
+    elem = _elem(dtype)
+    if out is None and tokens is bias_index is bias_value is mask is mask_row is None:
+        if (out_dtype is None or out_dtype is dtype) and (
+                token_count is repetition is presence is frequency is None):
+            return logits
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, tokens, token_count, repetition, presence, frequency,
+                                     bias_index, bias_value, mask, mask_row, out)):
+            return hbsjd_adjust_rows(logits, tokens, token_count, repetition, presence, frequency,
+                                     bias_index, bias_value, mask, mask_row, out, out_dtype)
     i32, f32, row = torch.int32, torch.float32, (rows,)
     n_tokens = ld_tokens = n_bias = ld_bias = n_masks = 0
-    at = dict.fromkeys(("tokens", "bias_index", "bias_value", "mask"))
+    tokens_at = index_at = value_at = mask_at = None
     if tokens is not None:
-        n_tokens, ld_tokens = _lists(tokens, "tokens", rows, i32, dev)
-        at["tokens"] = tokens.data_ptr()
+        n_tokens, ld_tokens, tokens_at = _lists(tokens, "tokens", rows, i32, dev)
     elif not (token_count is repetition is presence is frequency is None):
         raise ValueError("penalties without tokens")
-    if (bias_index is None) != (bias_value is None):
-        raise ValueError("bias_index and bias_value go together")
-    if bias_index is not None:
-        n_bias, ld_bias = _lists(bias_index, "bias_index", rows, i32, dev)
-        if _lists(bias_value, "bias_value", rows, f32, dev) != (n_bias, ld_bias):
+    if bias_index is not None and bias_value is not None:
+        n_bias, ld_bias, index_at = _lists(bias_index, "bias_index", rows, i32, dev)
+        n, ld_value, value_at = _lists(bias_value, "bias_value", rows, f32, dev)
+        if n != n_bias or ld_value != ld_bias:
             raise ValueError("bias_index and bias_value have to be laid out alike")
-        at["bias_index"], at["bias_value"] = bias_index.data_ptr(), bias_value.data_ptr()
+    elif bias_index is not bias_value:
+        raise ValueError("bias_index and bias_value go together")
     if mask is not None:
         n_masks = mask.shape[0]
-        at["mask"] = _vector(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
+        mask_at = _vector(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
         if not 1 <= n_masks <= _INT_MAX:
             raise ValueError(f"mask: {n_masks} masks")
-    a = _AdjustArgs(rows, V, elem, logits.data_ptr(), ld, at["tokens"], n_tokens, ld_tokens,
+    a = _AdjustArgs(rows, V, elem, logits.data_ptr(), ld, tokens_at, n_tokens, ld_tokens,
                     _vector(token_count, "token_count", row, i32, dev),
                     _vector(repetition, "repetition", row, f32, dev),
                     _vector(presence, "presence", row, f32, dev),
-                    _vector(frequency, "frequency", row, f32, dev), at["bias_index"],
-                    at["bias_value"], n_bias, ld_bias, at["mask"], n_masks,
-                    _vector(mask_row, "mask_row", row, i32, dev))
-    L = load_library()
-
-    def call(handle):
-        if out is None:
-            o = logits.new_empty((rows, V), dtype=out_dtype)
-            ld_out = V
-        else:
-            o = out
-            ld_out = _matrix(o, "out", logits)[2]
-            if out_dtype is not None and o.dtype is not out_dtype:
-                raise ValueError(f"out: expected {out_dtype}")
-        _check(L.hbsjd_adjust_rows(ctypes.byref(a), o.data_ptr(), _elem(o.dtype), ld_out, handle),
-               "hbsjd_adjust_rows")
-        return o
-
-    return _on_stream(call, dev, stream,
-                      (logits, tokens, token_count, repetition, presence, frequency, bias_index,
-                       bias_value, mask, mask_row, out))
+                    _vector(frequency, "frequency", row, f32, dev), index_at, value_at, n_bias,
+                    ld_bias, mask_at, n_masks, _vector(mask_row, "mask_row", row, i32, dev))
+    ld_out = V
+    if out is None:
+        out = logits.new_empty((rows, V), dtype=out_dtype)
+    else:
+        ld_out = _matrix(out, "out", logits)[2]
+        if out_dtype is not None and out.dtype is not out_dtype:
+            raise ValueError(f"out: expected {out_dtype}")
+    st = (_lib or load_library()).hbsjd_adjust_rows(a, out.data_ptr(), _elem(out.dtype), ld_out,
+                                                    torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_adjust_rows")
+    return out
 
 
 def hbsjd_mfma_probe(workgroups: int, iters: int, sink, stream=None):

@@ -507,9 +507,11 @@ def test_adjust_ignores_entries_and_counts_out_of_range():
                                                  bias=list(zip(bi[r], bv[r]))))
 
 
-def test_adjust_of_nothing_is_a_copy():
+def test_adjust_of_nothing():
     x = torch.randn(9, 501, device="cuda").to(torch.bfloat16)
-    assert torch.equal(P().hbsjd_adjust_rows(x), x)
+    assert P().hbsjd_adjust_rows(x) is x
+    out = torch.zeros_like(x)
+    assert P().hbsjd_adjust_rows(x, out=out) is out and torch.equal(out, x)
     assert torch.equal(P().hbsjd_adjust_rows(x, out_dtype=torch.float32), x.float())
 
 
