@@ -76,7 +76,7 @@ hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, 
         if (const char* why = workspace_problem(workspace, workspace_bytes,
                                                 top_logits_workspace(rows, V, K, elem)))
             return api_fail(HBSJD_EINVAL, why);
-        TopArgs a{rows, V, K, logits, elem, ld, 1.f / temperature, values, index, rest};
+        TopArgs a{rows, V, K, logits, elem, ld, 1.0 / temperature, values, index, rest};
         top_logits(a, workspace, (hipStream_t)stream);
         return launched("top_logits_rows");
     } catch (...) {

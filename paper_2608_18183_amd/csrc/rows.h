@@ -224,7 +224,7 @@ struct TopArgs {
     const void* logits;
     int32_t elem;
     int64_t ld;
-    float inv_tau;
+    double inv_tau;
     float* values;    // [rows][K]
     int32_t* index;   // [rows][K]
     float* rest;      // [rows]

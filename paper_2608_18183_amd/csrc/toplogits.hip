@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kPairs = 256;      // candidates compared with all others
 constexpr int kBinMost = 256;    // entries of one bin
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr double kLog2e = 1.4426950408889634;
 
 // larger for larger logits; -0 as +0, every NaN above +infinity
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -124,19 +124,28 @@ struct TopRow {
         return (int)(threadIdx.x & 63) < n_rests ? rests[threadIdx.x & 63] : -INFINITY;
     }
     // rest from the log of what the kernel itself left over; by whole wavefronts
-    __device__ __forceinline__ void put_rest(float own, float part) const {
+    __device__ __forceinline__ void put_rest(double own, float part) const {
         if (n_rests && own == own) {
-            const float m = fmaxf(own, wave_all(part, MaxOp()));
-            if (fabsf(m) == INFINITY) own = m;
-            else own = m + __logf(__expf(own - m) + wave_all(__expf(part - m), AddOp()));
+            const double m = fmax(own, (double)wave_all(part, MaxOp()));
+            if (fabs(m) == INFINITY) own = m;
+            else
+                own = m + (double)__logf(__expf((float)(own - m)) +
+                                         wave_all(__expf((float)((double)part - m)), AddOp()));
         }
-        if (threadIdx.x == 0) *rest = own;
+        if (threadIdx.x == 0) *rest = (float)own;
     }
 };
 
+// log of sum exp((z - ref) / tau) and its reference, joined: the two may nearly
+// cancel, so they are added in 64 bits (the log itself, of a number that is
+// neither tiny nor above V, is fp32's: 64-bit ones cost 8% of a batch's time)
+__device__ __forceinline__ double log_mass(float ref, double inv_tau, float sum) {
+    return sum > 0.f ? (double)ref * inv_tau + (double)__logf(sum) : -INFINITY;
+}
+
 // the digits' way, from memory, for rows of any kind
 template <int NT, typename T>
-__device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const TopRow& out,
+__device__ void top_by_digits(const T* z, int V, int K, double inv_tau, const TopRow& out,
                               uint64_t* kept, int* hist, float* red, int* word) {
     const int t = threadIdx.x;
     uint64_t prefix = 0;
@@ -176,7 +185,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
     float s = 0.f;
     for (int v = t; v < V; v += NT) {
         const float x = widen(z[v]);
-        if (ranked(x, out.entry(v)) < prefix) s += __expf((x - m) * inv_tau);
+        if (ranked(x, out.entry(v)) < prefix) s += __expf((x - m) * (float)inv_tau);
     }
     __syncthreads();
     s = block_all<NT>(s, red, AddOp());
@@ -196,7 +205,7 @@ __device__ void top_by_digits(const T* z, int V, int K, float inv_tau, const Top
     for (int k = t; k < K; k += NT) out.put(k, logit_of(kept[k]), index_of(kept[k]), K);
     if (t < 64) {
         const bool nan = kept[0] >> 32 == 0xFFFFFFFFu;
-        out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : m * inv_tau + __logf(s),
+        out.put_rest(nan ? __builtin_nanf("") : fabsf(m) == INFINITY ? m : log_mass(m, inv_tau, s),
                      out.part_rest());
     }
 }
@@ -223,7 +232,7 @@ template <int NV> __device__ __forceinline__ void opaque(u32x4 (&x)[NV]) {
 }
 
 template <typename T, int NT, int NV, int Cap, bool Join>
-__device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau, const TopRow& out) {
+__device__ __forceinline__ void top_row(const T* z, int V, int K, double inv_tau, const TopRow& out) {
     constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
     static_assert(N >= 8, "eight groups a thread");
     using Cand = Candidate<T>;
@@ -239,7 +248,7 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
     __shared__ int word[4];
     __shared__ float s_last;
     const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
-    const float c2 = inv_tau * kLog2e;
+    const float c2 = (float)(inv_tau * kLog2e);
 
     // The thread's first vector. A join's vectors are nearly in order: they are
     // dealt out one by one, so that every wavefront has its share of the largest.
@@ -518,11 +527,12 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
                 over += __builtin_amdgcn_exp2f((Cand::logit(me[n]) - last) * c2);
         over = block_all<NT>(over, red[2], AddOp());
     }
-    // A sum too far below its reference: again, relative to the largest term.
-    // (With candidates left over the mass below the pivot is at most V times the
-    // least of them, so only without any does it matter.)
+    // A sum far below its reference, where the exponents' roundings are coarse:
+    // again, relative to the largest term. (With candidates left over the mass
+    // below the pivot is at most V times the least of them, so only without any
+    // does it matter.)
     float ref_below = ref, ref_over = last;
-    if (C > K ? over < 0x1p-60f : below < 0x1p-60f) {
+    if (C > K ? over < 0x1p-6f : below < 0x1p-6f) {
         const uint64_t bound = C > K ? (uint64_t)last_image << 32 : (uint64_t)order_of(from) << 32;
         float m = -INFINITY, s = 0.f;
         for (int v = t; v < V; v += NT) {
@@ -541,10 +551,10 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, float inv_tau,
         over = 0.f;
     }
     if (t < 64) {
-        const float a = below > 0.f ? ref_below * inv_tau + __logf(below) : -INFINITY;
-        const float b = over > 0.f ? ref_over * inv_tau + __logf(over) : -INFINITY;
-        const float m = fmaxf(a, b);
-        out.put_rest(m == -INFINITY ? m : m + __logf(__expf(a - m) + __expf(b - m)), part_rest);
+        const double a = log_mass(ref_below, inv_tau, below), b = log_mass(ref_over, inv_tau, over);
+        const double m = fmax(a, b);
+        const float sum = __expf((float)(a - m)) + __expf((float)(b - m));
+        out.put_rest(m == -INFINITY ? m : m + (double)__logf(sum), part_rest);
     }
 }
 

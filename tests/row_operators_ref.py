@@ -87,6 +87,11 @@ def distill(z, values, index, rest, w, tau, alpha, beta):
         err = alpha * (qa + pv) * 2 * dv
         if beta:
             err = err + beta * np.where(qa > 0, qa * (np.abs(cv - kl_q) * 2 * dv + dv + err_q), 0.0)
+        # the hardware's exp2 gives 0 below 2^-126: an unlisted entry's e_v may be
+        # missing, which its factor (alpha (q_0 - P_0) + beta q_0 (c_0 - R)) / s_0, with
+        # q_0, P_0 <= 1 <= s_0, makes at most this; a listed one's q likewise
+        err = err + 2.0 ** -126 * (alpha + beta * (1 + np.abs(np.where(np.isfinite(cv), cv - kl_q, 0.0))
+                                                   if beta else 0.0))
         g_err = abs(w) / tau * err + 4 * U * np.abs(g)
     return w * loss, g, abs(w) * loss_err, g_err
 

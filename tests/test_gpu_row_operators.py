@@ -134,6 +134,19 @@ def test_top_logits_far_from_zero(V):
             check_top(x.astype(np.float64), P().hbsjd_top_logits_rows(dev(x), k, temperature=tau), k, tau)
 
 
+@pytest.mark.parametrize("V", [3, 70, 3000, 20000])
+def test_top_logits_rest_far_below_the_listed(V):
+    """A confident row: the others' mass lies 5 to 80 below the listed logits, and
+    its log keeps the digits that its own size asks for."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 0.3, (8, V)).astype(np.float32)
+    x[:, 1] = [2.0, 4.0, 8.0, 14.8, 20.0, 30.0, 40.0, 80.0]
+    x[4:, 2] = x[4:, 1] - 1.5
+    for k in (1, 2):
+        for tau in (0.5, 1.0):
+            check_top(x.astype(np.float64), P().hbsjd_top_logits_rows(dev(x), k, temperature=tau), k, tau)
+
+
 def test_top_logits_of_rows_with_nan_and_infinity():
     rng = np.random.default_rng(0)
     x = rng.normal(0, 1, (4, 500)).astype(np.float32)
