@@ -377,6 +377,22 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, double inv_tau
     }
     if (xe >= from) cand[slot++] = Cand::of(xe, out.entry(sp.edge(t, V)));
 
+    // fewer than K entries above -infinity: then the first of those at it
+    for (int base = 0, filled = C; __builtin_expect(filled < K, 0) && base < V; base += NT) {
+        __syncthreads();
+        const int v = base + t;
+        const uint64_t at = __ballot(v < V && widen(z[min(v, V - 1)]) == -INFINITY);
+        if (lane == 0) s_count[wv] = __popcll(at);
+        __syncthreads();
+        int k = filled + __popcll(at & ((1ull << lane) - 1));
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < wv) k += s_count[w];
+            filled += s_count[w];
+        }
+        if ((at >> lane & 1) && k < K) out.put(k, -INFINITY, out.entry(v), K);
+    }
+
     // ---- 3. places
     constexpr int M = Cap / NT;   // candidates a thread looks after
     static_assert(M >= 1 && M * NT == Cap, "");
@@ -495,22 +511,6 @@ __device__ __forceinline__ void top_row(const T* z, int V, int K, double inv_tau
         __syncthreads();
         for (int k = t; k < min(K, C); k += NT) out.put(k, Cand::logit(cand[k]), Cand::index(cand[k]), K);
     }
-    // fewer than K entries above -infinity: then the first of those at it
-    for (int base = 0, filled = C; filled < K && base < V; base += NT) {
-        __syncthreads();
-        const int v = base + t;
-        const uint64_t at = __ballot(v < V && widen(z[min(v, V - 1)]) == -INFINITY);
-        if (lane == 0) s_count[wv] = __popcll(at);
-        __syncthreads();
-        int k = filled + __popcll(at & ((1ull << lane) - 1));
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (w < wv) k += s_count[w];
-            filled += s_count[w];
-        }
-        if ((at >> lane & 1) && k < K) out.put(k, -INFINITY, out.entry(v), K);
-    }
-
     // ---- the mass of the others: below the pivot, and the candidates left over
     const float last = uniform(s_last);
     const uint32_t last_image = order_of(last);
