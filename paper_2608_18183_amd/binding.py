@@ -432,15 +432,24 @@ def _matrix(t, what: str, like=None):
     return rows, V, ld
 
 
-def _vector(t, what: str, shape, dtype, device):
+def _address(t, what: str, shape, dtype, device):
     """The address of a contiguous device tensor of this shape and type, or None."""
     if t is None:
         return None
-    if not isinstance(t, _torch.Tensor) or t.shape != shape or t.dtype is not dtype:
-        raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}")
-    if t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous tensor on {device}")
-    return t.data_ptr()
+    if (isinstance(t, _torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == device.index and t.is_contiguous()):
+        return t.data_ptr()
+    raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _per_row(t, what: str, rows: int, dtype, device):
+    """The same for a number a row."""
+    if t is None:
+        return None
+    if (isinstance(t, _torch.Tensor) and t.dtype is dtype and t.dim() == 1 and t.numel() == rows
+            and t.get_device() == device.index and t.is_contiguous()):
+        return t.data_ptr()
+    raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape ({rows},) on {device}")
 
 
 def _lists(t, what: str, rows: int, dtype, device):
@@ -513,9 +522,9 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
         at = values.data_ptr(), index.data_ptr(), rest.data_ptr()
     else:
         values, index, rest = out
-        at = (_vector(values, "values", (rows, k), torch.float32, dev),
-              _vector(index, "index", (rows, k), torch.int32, dev),
-              _vector(rest, "rest", (rows,), torch.float32, dev))
+        at = (_address(values, "values", (rows, k), torch.float32, dev),
+              _address(index, "index", (rows, k), torch.int32, dev),
+              _address(rest, "rest", (rows,), torch.float32, dev))
     L = _lib or load_library()
     ws, nbytes = None, 0
     if V > _WHOLE_ROWS:
@@ -546,17 +555,17 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
                                           reverse_weight, row_weight, grad)
     if values is None or index is None or values.dim() != 2:
         raise ValueError(f"values and index: expected tensors of shape [{rows}, K]")
-    shape, row, f32 = values.shape, (rows,), torch.float32
+    shape, f32 = values.shape, torch.float32
     K = min(shape[1], _INT_MAX)
     a = _DistillArgs(rows, V, K, logits.data_ptr(), ld, elem, temperature,
-                     _vector(values, "values", (rows, K), f32, dev),
-                     _vector(index, "index", shape, torch.int32, dev),
-                     _vector(rest, "rest", row, f32, dev), forward_weight, reverse_weight,
-                     _vector(row_weight, "row_weight", row, f32, dev))
-    loss = logits.new_empty(row, dtype=f32)
+                     _address(values, "values", (rows, K), f32, dev),
+                     _address(index, "index", shape, torch.int32, dev),
+                     _per_row(rest, "rest", rows, f32, dev), forward_weight, reverse_weight,
+                     _per_row(row_weight, "row_weight", rows, f32, dev))
+    loss = logits.new_empty((rows,), dtype=f32)
     ld_grad, address = V, None
     if grad is True:
-        grad = logits.new_empty((rows, V))
+        grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
         address = grad.data_ptr()
     elif grad is False or grad is None:
         grad = None
@@ -603,7 +612,7 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
                                      bias_index, bias_value, mask, mask_row, out)):
             return hbsjd_adjust_rows(logits, tokens, token_count, repetition, presence, frequency,
                                      bias_index, bias_value, mask, mask_row, out, out_dtype)
-    i32, f32, row = torch.int32, torch.float32, (rows,)
+    i32, f32 = torch.int32, torch.float32
     n_tokens = ld_tokens = n_bias = ld_bias = n_masks = 0
     tokens_at = index_at = value_at = mask_at = None
     if tokens is not None:
@@ -619,18 +628,18 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
         raise ValueError("bias_index and bias_value go together")
     if mask is not None:
         n_masks = mask.shape[0]
-        mask_at = _vector(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
+        mask_at = _address(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
         if not 1 <= n_masks <= _INT_MAX:
             raise ValueError(f"mask: {n_masks} masks")
     a = _AdjustArgs(rows, V, elem, logits.data_ptr(), ld, tokens_at, n_tokens, ld_tokens,
-                    _vector(token_count, "token_count", row, i32, dev),
-                    _vector(repetition, "repetition", row, f32, dev),
-                    _vector(presence, "presence", row, f32, dev),
-                    _vector(frequency, "frequency", row, f32, dev), index_at, value_at, n_bias,
-                    ld_bias, mask_at, n_masks, _vector(mask_row, "mask_row", row, i32, dev))
+                    _per_row(token_count, "token_count", rows, i32, dev),
+                    _per_row(repetition, "repetition", rows, f32, dev),
+                    _per_row(presence, "presence", rows, f32, dev),
+                    _per_row(frequency, "frequency", rows, f32, dev), index_at, value_at, n_bias,
+                    ld_bias, mask_at, n_masks, _per_row(mask_row, "mask_row", rows, i32, dev))
     ld_out = V
     if out is None:
-        out = logits.new_empty((rows, V), dtype=out_dtype)
+        out = torch.empty_like(logits, dtype=out_dtype, memory_format=torch.contiguous_format)
     else:
         ld_out = _matrix(out, "out", logits)[2]
         if out_dtype is not None and out.dtype is not out_dtype:
