@@ -334,9 +334,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
 // Rows too long for a workgroup's registers, or long and few: `parts` workgroups
 // a row, in two launches. The first leaves each part's unlisted maximum and sum,
 // and the listed entries' logits, in the workspace; the second joins them (every
-// part's workgroup works the classes out for itself) and writes the gradient. The
-// part is read again then, mostly from the caches: rows are taken in slabs that
-// fit them.
+// part's workgroup works the classes out for itself) and writes the gradient,
+// reading the part again. (Rows in slabs that the last-level cache holds make the
+// second reading cheaper and the whole slower, by the launches' ends: 2000 bf16
+// rows of 200000 in slabs of 192 MB 566 us, of 384 MB 535, at once 515.)
 struct PartsArgs {
     int parts, len;
     float* zk;       // [rows of the slab][K]
@@ -427,20 +428,21 @@ constexpr int kPart = 16384;   // entries of a part at most
 
 inline size_t part_row_bytes(const Plan& p, int K) { return ((size_t)K + 3 * (size_t)p.parts) * 4; }
 
-// Parts where a workgroup cannot hold the row, and for long rows that are fewer
-// than the CUs: then enough of them for two workgroups a CU, of 4096 entries at
-// least.
+// Parts where a workgroup cannot hold the row, and for rows above 128 KB that are
+// few: then enough of them for two workgroups a CU, of 4096 entries at least. (64
+// fp16 rows of 128257: 24 us in parts, 32 held; 140 bf16 rows of 100000: 33 and 31;
+// 200 fp32 rows of 60000: 40 and 27; 900 of them 159 and 116, though the largest
+// held rows spill; 140 fp32 rows of 20000: 24 and 15.)
 Plan plan_of(int64_t rows, int V, int K, int32_t elem) {
     Plan p;
     const int64_t size = elem_size(elem);
-    const int64_t held = 1024 * (elem == HBSJD_ELEM_F32 ? 8 : 16) * (16 / size);
-    if (V <= kPart || (V <= held && rows >= 256)) return p;
+    const int64_t held = 1024 * 16 * (16 / size);
+    if (V * size <= 128 << 10 || (V <= held && rows >= 112)) return p;
     p.parts = (V + kPart - 1) / kPart;
     while (rows * p.parts < 512 && V / (2 * p.parts) >= 4096) p.parts *= 2;   // 64 at most: a lane each
     p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (V + p.len - 1) / p.len;
-    // a slab's logits and gradient together stay within the last-level cache
-    p.slab = std::max<int64_t>(1, (96 << 20) / (V * size));
+    p.slab = std::max<int64_t>(1, (64 << 20) / (int64_t)part_row_bytes(p, K));
     p.slab = std::min(p.slab, rows);
     return p;
 }
@@ -476,7 +478,7 @@ template <typename T> void go(const DistillArgs& a, void* ws, hipStream_t s) {
     else if (vecs <= 256 * 8) HELD(256, 8);
     else if (vecs <= 512 * 8) HELD(512, 8);
     else if (vecs <= 1024 * 8) HELD(1024, 8);
-    else if constexpr (sizeof(T) == 2) HELD(1024, 16);
+    else HELD(1024, 16);
 #undef HELD
 }
 

@@ -46,12 +46,14 @@ __device__ __forceinline__ int index_of(uint64_t c) { return (int)~(uint32_t)c; 
 __device__ __forceinline__ float logit_of(uint64_t c) { return value_of((uint32_t)(c >> 32)); }
 
 // A candidate as one number: an order-preserving image of its logit above its
-// complemented index. 16-bit logits have 16-bit images, and with the 14 bits of
-// an index within a part the number takes 32 bits: half the LDS, and comparisons
-// at full rate (K = 2000 of 16384 bf16 entries, where equal logits share bins:
+// complemented index. 16-bit logits have 16-bit images, and with the 14 or 15 bits
+// of an index within what a workgroup holds (Held entries; no more bits than that:
+// equal logits are binned by their index) the number takes 32 bits: half the LDS,
+// and comparisons at full rate (K = 2000 of 16384 bf16 entries, where equal logits share bins:
 // 54 us with 64 bits).
-constexpr int kPart = 16384;   // entries of a part at most
-template <typename T> struct Candidate {
+constexpr int kWhole = 32768;  // entries of a row that goes whole at most
+constexpr int kPart = 16384;   // of a part
+template <typename T, int Held> struct Candidate {
     using Key = uint64_t;
     static constexpr int kBins = 1024;
     __device__ __forceinline__ static Key of(float x, int v) { return ranked(x, v); }
@@ -62,8 +64,10 @@ template <typename T> struct Candidate {
     __device__ __forceinline__ static uint32_t least(float x) { return order_of(x); }
     __device__ __forceinline__ static uint32_t most(float x) { return order_of(x); }
 };
-template <typename T> struct Candidate16 {
+template <typename T, int Held> struct Candidate16 {
     using Key = uint32_t;
+    static constexpr int kShift = Held <= 16384 ? 14 : 15, kLow = (1 << kShift) - 1;
+    static_assert(Held <= 1 << kShift, "an index has to fit");
     static constexpr int kBins = 2048;
     __device__ __forceinline__ static uint32_t order(float x) {
         uint32_t u;
@@ -71,19 +75,19 @@ template <typename T> struct Candidate16 {
         else u = __builtin_bit_cast(uint16_t, (_Float16)(x + 0.f));
         return u & 0x8000u ? ~u & 0xFFFFu : u | 0x8000u;
     }
-    __device__ __forceinline__ static Key of(float x, int v) { return order(x) << 14 | (kPart - 1 - v); }
-    __device__ __forceinline__ static int index(Key c) { return kPart - 1 - (int)(c & (kPart - 1)); }
+    __device__ __forceinline__ static Key of(float x, int v) { return order(x) << kShift | (kLow - v); }
+    __device__ __forceinline__ static int index(Key c) { return kLow - (int)(c & kLow); }
     __device__ __forceinline__ static float logit(Key c) {
-        const uint32_t k = c >> 14, u = k & 0x8000u ? k & 0x7FFFu : ~k & 0xFFFFu;
+        const uint32_t k = c >> kShift, u = k & 0x8000u ? k & 0x7FFFu : ~k & 0xFFFFu;
         if constexpr (std::is_same_v<T, Bf16>) return __uint_as_float(u << 16);
         else return (float)__builtin_bit_cast(_Float16, (uint16_t)u);
     }
     __device__ __forceinline__ static uint32_t image(Key c) { return c; }
-    __device__ __forceinline__ static uint32_t least(float x) { return order(x) << 14; }
-    __device__ __forceinline__ static uint32_t most(float x) { return order(x) << 14 | (kPart - 1); }
+    __device__ __forceinline__ static uint32_t least(float x) { return order(x) << kShift; }
+    __device__ __forceinline__ static uint32_t most(float x) { return order(x) << kShift | kLow; }
 };
-template <> struct Candidate<Bf16> : Candidate16<Bf16> {};
-template <> struct Candidate<F16> : Candidate16<F16> {};
+template <int Held> struct Candidate<Bf16, Held> : Candidate16<Bf16, Held> {};
+template <int Held> struct Candidate<F16, Held> : Candidate16<F16, Held> {};
 
 // room for candidates
 constexpr int kFew = 1024, kMany = 4096;
@@ -235,7 +239,7 @@ template <typename T, int NT, int NV, int Cap, bool Join>
 __device__ __forceinline__ void top_row(const T* z, int V, int K, double inv_tau, const TopRow& out) {
     constexpr int E = kVec<T>, N = NV * E, NW = NT / 64;
     static_assert(N >= 8, "eight groups a thread");
-    using Cand = Candidate<T>;
+    using Cand = Candidate<T, NT * N>;
     using Key = typename Cand::Key;
     constexpr int kBins = Cand::kBins;
     // (the digits' way keeps up to K 64-bit numbers there)
@@ -600,11 +604,12 @@ struct Plan {
 };
 inline size_t part_row_bytes(const Plan& p, int K) { return (size_t)p.parts * (8 * (size_t)list_room(K) + 4); }
 
-// Rows of more entries than a workgroup holds go in parts; where rows are few,
+// Rows of more than kWhole entries go in parts, and many fp32 ones of more than
+// kPart (2000 of 25000, K 64: 74 us, whole 87; 100 of 30000: 20 and 13); where rows are few,
 // in more and smaller ones, as long as the join stays the smaller work.
-Plan plan_of(int64_t rows, int V, int K) {
+Plan plan_of(int64_t rows, int V, int K, int32_t elem) {
     Plan p;
-    if (V <= kPart) return p;
+    if (V <= kPart || (V <= kWhole && (elem != HBSJD_ELEM_F32 || rows <= 512))) return p;
     p.parts = (V + kPart - 1) / kPart;
     while (rows * p.parts < 256 && V / (2 * p.parts) >= std::max(4096, 8 * K) && 2 * p.parts * K <= 8192)
         p.parts *= 2;
@@ -621,29 +626,26 @@ Plan plan_of(int64_t rows, int V, int K) {
 // 2 K groups, unless all of the row's entries may be candidates.
 template <typename T, typename F> void by_size(int V, int K, int least, F f) {
     using std::integral_constant;
-    const int vecs = V / kVec<T>;
     auto fits = [&](auto nt, auto nv) {
         constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-        return NT >= least && vecs <= NT * NV && (NT * 8 >= 2 * K || V <= (NT == 64 ? kFew : kMany));
+        return NT >= least && V <= NT * NV * kVec<T> && (NT * 8 >= 2 * K || V <= (NT == 64 ? kFew : kMany));
     };
 #define FITS(nt, nv) fits(integral_constant<int, nt>{}, integral_constant<int, nv>{})
 #define CALL(nt, nv, cap) \
     f(integral_constant<int, nt>{}, integral_constant<int, nv>{}, integral_constant<int, cap>{})
     const bool few = K <= 256 || V <= kFew;
-    if (FITS(64, 2) && V <= kFew) CALL(64, 2, kFew);
+    if (FITS(64, 2)) CALL(64, 2, kFew);
     else if (FITS(64, 8)) CALL(64, 8, kFew);
     else if (FITS(256, 4)) { if (few) CALL(256, 4, kFew); else CALL(256, 4, kMany); }
     else if (FITS(512, 4)) { if (few) CALL(512, 4, kFew); else CALL(512, 4, kMany); }
-    else if constexpr (sizeof(T) == 4) {
-        if (FITS(512, 8)) { if (few) CALL(512, 8, kFew); else CALL(512, 8, kMany); }
-        else CALL(1024, 8, kMany);
-    }
+    else if (FITS(512, 8)) { if (few) CALL(512, 8, kFew); else CALL(512, 8, kMany); }
+    else if constexpr (sizeof(T) == 4) CALL(1024, 8, kMany);
 #undef FITS
 #undef CALL
 }
 
 template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
-    const Plan plan = plan_of(a.rows, a.V, a.K);
+    const Plan plan = plan_of(a.rows, a.V, a.K, a.elem);
     if (!plan.parts) {
         by_size<T>(a.V, a.K, 64, [&](auto nt, auto nv, auto cap) {
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
@@ -661,7 +663,7 @@ template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
         const int64_t n = std::min(plan.slab, a.rows - r0);
         by_size<T>(p.len, a.K, 256, [&](auto nt, auto nv, auto cap) {
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value, Cap = decltype(cap)::value;
-            if constexpr (NT >= 256 && NT <= 512)
+            if constexpr (NT >= 256 && NT * NV * kVec<T> <= kPart)
                 hipLaunchKernelGGL((k_top_part<T, NT, NV, Cap>), dim3((unsigned)(n * p.parts)), dim3(NT),
                                    0, s, a, p, r0);
         });
@@ -675,8 +677,8 @@ template <typename T> void go(const TopArgs& a, void* ws, hipStream_t s) {
 
 }  // namespace
 
-size_t top_logits_workspace(int64_t rows, int V, int K, int32_t) {
-    const Plan p = plan_of(rows, V, K);
+size_t top_logits_workspace(int64_t rows, int V, int K, int32_t elem) {
+    const Plan p = plan_of(rows, V, K, elem);
     return p.parts ? p.slab * part_row_bytes(p, K) : 0;
 }
 
