@@ -43,8 +43,8 @@ inline size_t entries_bytes(int V, int K) { return ((size_t)(V + 31) / 32 + 3 * 
 
 // Fetches the answer and marks its entries that lie among the V from `first` on.
 // Their logits are gathered here (before anything of the gradient is written: it
-// may take the logits' place), or read from `gathered`. mt and mk: the largest
-// t_k / tau and z_k that this thread has seen.
+// may take the logits' place), or read from `gathered`. mt and mk: the largest t_k and
+// z_k that this thread has seen.
 template <int NT, typename T>
 __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* z, const Span& sp,
                                       int first, int V, const Entries& e, int* bad, float* gathered,
@@ -72,7 +72,7 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
             if (!gather || !gathered) {
                 e.zk[k] = y;
                 mk = fmaxf(mk, y);
-                mt = fmaxf(mt, x * a.inv_tau);
+                mt = fmaxf(mt, x);
             }
         }
         e.entry[k] = v;
@@ -102,7 +102,10 @@ struct RowStats {
 // below the logs it is made of keeps its digits: a and b are differences in 64
 // bits, c is formed with any D_f near D, the sums of P c and q c are held in 64
 // bits, and D - D_f, which every entry shares, joins them at the end. One
-// wavefront works out the logs in 64 bits; the exponentials are fp32's.
+// wavefront works out the logs in 64 bits; the exponentials are fp32's. The
+// largest of either side has the exponent 0 exactly, whatever the temperature: the
+// logits are subtracted before they are divided (a quotient's rounding in fp32 is
+// larger than exp's range from 1e9 on, and one in 64 bits from 1e18 on).
 // Leaves alpha (q - P) + beta q c in zk and beta q in tk for listed_gradient().
 template <int NT>
 __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries& e, float rest, float m0,
@@ -111,7 +114,13 @@ __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries&
                                             double* shared) {
     const float m = fmaxf(m0, mk);
     auto student = [&](float z) { return ((double)z - (double)m) * a.inv_tau_d; };
-    auto teacher = [&](float t) { return (double)t * a.inv_tau_d - (double)mt; };
+    // the teacher's terms relative to the larger of its largest logit and `rest`;
+    // an infinite or NaN `rest` that is the larger leaves NaN
+    const double top = (double)mt * a.inv_tau_d, from = mt == -INFINITY ? 0.0 : (double)mt;
+    const bool listed_top = top >= (double)rest;
+    const double shift = listed_top ? 0.0 : from * a.inv_tau_d - (double)rest;
+    const double a0 = (double)rest - (listed_top ? top : (double)rest);
+    auto teacher = [&](float t) { return ((double)t - from) * a.inv_tau_d + shift; };
     float s[3] = {s0_part, 0.f, 0.f};
     for (int k = threadIdx.x; k < a.K; k += NT) {
         if (e.entry[k] < 0) continue;
@@ -119,7 +128,7 @@ __device__ __forceinline__ RowStats classes(const DistillArgs& a, const Entries&
         s[2] += exp_of(teacher(e.tk[k]));
     }
     block_all<NT, 3>(s, red, AddOp());
-    const double b0_ref = student(m0), a0 = (double)rest - (double)mt;
+    const double b0_ref = student(m0);
     const float s0 = s[0], s0m = s0 * exp_of(b0_ref);
     const float rest_e = a.rest ? exp_of(a0) : 0.f;
     const float sz = s0m + s[1], st = s[2] + rest_e;
@@ -313,7 +322,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     for (int i = t; i < (a.V + 31) / 32; i += NT) e.listed[i] = 0;
     if (t == 0) bad = 0;
     __syncthreads();
-    float mm[3] = {-INFINITY, -INFINITY, rest};   // maxima: unlisted, listed, teacher
+    float mm[3] = {-INFINITY, -INFINITY, -INFINITY};   // maxima: unlisted, listed, teacher's listed
     fetch<NT>(a, r, z, h.sp, 0, a.V, e, &bad, nullptr, true, mm[2], mm[1]);
     __syncthreads();
     mm[0] = h.mask(e.listed);
@@ -382,7 +391,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     for (int i = t; i < (V + 31) / 32; i += NT) e.listed[i] = 0;
     if (t == 0) bad = 0;
     __syncthreads();
-    float mm[3] = {-INFINITY, -INFINITY, rest};
+    float mm[3] = {-INFINITY, -INFINITY, -INFINITY};
     fetch<NT>(a, r, z, h.sp, first, V, e, &bad, zk, !Second, mm[2], mm[1]);
     __syncthreads();
     if constexpr (!Second) {
