@@ -496,6 +496,12 @@ class _OnStream:
         self._context.__exit__(*exc)
 
 
+def _written(*tensors):
+    """Tells autograd that a call has written these tensors of the caller's: a
+    backward pass that saved one of them raises instead of reading what it holds now."""
+    _torch.autograd.graph.increment_version(tensors)
+
+
 def _here(device, stream) -> bool:
     """Whether a call runs on the current device's current stream."""
     return stream is None and device.index == _torch._C._cuda_getDevice()
@@ -505,7 +511,8 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
     """logits: device tensor [rows, V], fp32, bf16 or fp16, with any row stride.
     Returns device tensors (values fp32 [rows, k], index int32 [rows, k], rest
     fp32 [rows]), written into `out` when given. Asynchronous on `stream` (the
-    current one by default), as are the two calls below."""
+    current one by default), as are the two calls below. Autograd records none of
+    the three; to it, tensors of the caller's that they write are changed in place."""
     torch = _torch or _load_torch()
     rows, V, ld = _matrix(logits, "logits")
     elem, dev = _elem(logits.dtype), logits.device
@@ -535,6 +542,8 @@ def hbsjd_top_logits_rows(logits, k: int, temperature: float = 1.0, stream=None,
                                  torch._C._cuda_getCurrentRawStream(dev.index))
     if st:
         _check(st, "hbsjd_top_logits_rows")
+    if out is not None:
+        _written(values, index, rest)
     return values, index, rest
 
 
@@ -563,7 +572,7 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
                      _per_row(rest, "rest", rows, f32, dev), forward_weight, reverse_weight,
                      _per_row(row_weight, "row_weight", rows, f32, dev))
     loss = logits.new_empty((rows,), dtype=f32)
-    ld_grad, address = V, None
+    ld_grad, address, given = V, None, False
     if grad is True:
         grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
         address = grad.data_ptr()
@@ -573,7 +582,7 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
         ld_grad = _matrix(grad, "grad", logits)[2]
         if grad.dtype is not logits.dtype:
             raise ValueError("grad: expected the logits' type")
-        address = grad.data_ptr()
+        address, given = grad.data_ptr(), True
     L = _lib or load_library()
     ws, nbytes = None, 0
     if V > _WHOLE_ROWS:
@@ -584,6 +593,8 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
                                   torch._C._cuda_getCurrentRawStream(dev.index))
     if st:
         _check(st, "hbsjd_distill_top_rows")
+    if given:
+        _written(grad)
     return loss, grad
 
 
@@ -637,8 +648,8 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
                     _per_row(presence, "presence", rows, f32, dev),
                     _per_row(frequency, "frequency", rows, f32, dev), index_at, value_at, n_bias,
                     ld_bias, mask_at, n_masks, _per_row(mask_row, "mask_row", rows, i32, dev))
-    ld_out = V
-    if out is None:
+    ld_out, given = V, out is not None
+    if not given:
         out = torch.empty_like(logits, dtype=out_dtype, memory_format=torch.contiguous_format)
     else:
         ld_out = _matrix(out, "out", logits)[2]
@@ -648,6 +659,8 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
                                                     torch._C._cuda_getCurrentRawStream(dev.index))
     if st:
         _check(st, "hbsjd_adjust_rows")
+    if given:
+        _written(out)
     return out
 
 
