@@ -609,7 +609,8 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     new tensor of out_dtype (the logits' type by default; fp32 is what
     hbsjd_transform_rows takes), or `out`, which may be the logits. With nothing
     to adjust, no `out` and the logits' type it returns the logits themselves, as
-    a tensor's to() does."""
+    a tensor's to() does (detached where they require a gradient, since none
+    reaches them through any other call either): clone them before writing there."""
     torch = _torch or _load_torch()
     rows, V, ld = _matrix(logits, "logits")
     dtype, dev = logits.dtype, logits.device
@@ -617,7 +618,7 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     if out is None and tokens is bias_index is bias_value is mask is mask_row is None:
         if (out_dtype is None or out_dtype is dtype) and (
                 token_count is repetition is presence is frequency is None):
-            return logits
+            return logits.detach() if logits.requires_grad else logits
     if not _here(dev, stream):
         with _OnStream(dev, stream, (logits, tokens, token_count, repetition, presence, frequency,
                                      bias_index, bias_value, mask, mask_row, out)):

@@ -1,5 +1,4 @@
-"""Autograd and the row operators: it sees what they write."""
-import numpy as np
+"""Autograd records none of the row operators, and sees what they write."""
 import pytest
 
 from tests import row_operators_ref as ref
@@ -61,6 +60,19 @@ def test_every_output_is_marked_and_no_input():
     P().hbsjd_adjust_rows(x, tokens=out[1], frequency=out[2], stream=s)
     s.synchronize()
     assert [t._version for t in (x, *out)] == at and g._version > 0
+
+
+def test_results_are_no_part_of_the_graph():
+    """Whether or not there is anything to adjust, no gradient reaches the logits."""
+    x = torch.randn(3, 40, device="cuda", requires_grad=True)
+    pen = dict(tokens=torch.zeros(3, dtype=torch.int32, device="cuda"),
+               presence=torch.ones(3, device="cuda"))
+    for kw in ({}, pen, dict(out_dtype=torch.float32), dict(out=torch.empty(3, 40, device="cuda"))):
+        assert not P().hbsjd_adjust_rows(x, **kw).requires_grad
+    y = P().hbsjd_adjust_rows(x)
+    assert torch.equal(y, x) and y.data_ptr() == x.data_ptr()
+    assert not any(t.requires_grad for t in P().hbsjd_top_logits_rows(x, 3))
+    assert not any(t.requires_grad for t in P().hbsjd_distill_top_rows(x, *answer_of(x)))
 
 
 def test_a_model_takes_its_gradient_in_the_logits_place():
