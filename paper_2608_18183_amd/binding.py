@@ -562,7 +562,7 @@ def hbsjd_distill_top_rows(logits, values, index, rest=None, temperature: float 
         with _OnStream(dev, stream, (logits, values, index, rest, row_weight, grad)):
             return hbsjd_distill_top_rows(logits, values, index, rest, temperature, forward_weight,
                                           reverse_weight, row_weight, grad)
-    if values is None or index is None or values.dim() != 2:
+    if not isinstance(values, torch.Tensor) or values.dim() != 2 or index is None:
         raise ValueError(f"values and index: expected tensors of shape [{rows}, K]")
     shape, f32 = values.shape, torch.float32
     K = min(shape[1], _INT_MAX)
@@ -639,6 +639,8 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     elif bias_index is not bias_value:
         raise ValueError("bias_index and bias_value go together")
     if mask is not None:
+        if not isinstance(mask, torch.Tensor) or mask.dim() != 2:
+            raise ValueError(f"mask: expected a tensor of shape [masks, {(V + 31) // 32}]")
         n_masks = mask.shape[0]
         mask_at = _address(mask, "mask", (n_masks, (V + 31) // 32), i32, dev)
         if not 1 <= n_masks <= _INT_MAX:
