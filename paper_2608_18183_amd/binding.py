@@ -490,10 +490,10 @@ class _OnStream:
         return self._stream.cuda_stream
 
     def __exit__(self, *exc):
-        for t in self._tensors:
-            if isinstance(t, _torch.Tensor):
-                t.record_stream(self._stream)
         self._context.__exit__(*exc)
+        for t in self._tensors:   # what a refused call was given may be anything
+            if isinstance(t, _torch.Tensor) and t.is_cuda:
+                t.record_stream(self._stream)
 
 
 def _written(*tensors):

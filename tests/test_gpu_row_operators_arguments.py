@@ -36,3 +36,23 @@ def test_arguments_that_are_no_tensors(what, other_stream):
         with pytest.raises(ValueError):
             P().hbsjd_top_logits_rows(x, 8, out=bad, stream=stream)
     torch.cuda.synchronize()
+
+
+def test_a_refused_call_leaves_the_current_stream():
+    """Refused for a tensor in host memory, on a stream that is not the current one."""
+    x = torch.randn(4, 64, device="cuda")
+    v, i, rest = out = P().hbsjd_top_logits_rows(x, 8)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = torch.cuda.current_stream()
+    for f in (lambda: P().hbsjd_top_logits_rows(x, 8, out=(v, i.cpu(), rest), stream=s),
+              lambda: P().hbsjd_distill_top_rows(x, v.cpu(), i, rest, stream=s),
+              lambda: P().hbsjd_distill_top_rows(x, v, i, rest, grad=x.cpu(), stream=s),
+              lambda: P().hbsjd_adjust_rows(x, tokens=i.cpu(), frequency=rest, stream=s)):
+        with pytest.raises(ValueError):
+            f()
+        assert torch.cuda.current_stream() == before
+    assert all(a.data_ptr() == b.data_ptr() for a, b in
+               zip(P().hbsjd_top_logits_rows(x, 8, out=out, stream=s), out))
+    assert torch.cuda.current_stream() == before
+    torch.cuda.synchronize()
