@@ -330,8 +330,8 @@ hbsjd_status hbsjd_top_logits_rows(int64_t rows, int32_t V, const void* logits, 
  *   L_r  = forward_weight KL(P || q) + reverse_weight KL(q || P)
  *   loss[r]    = w_r L_r
  *   grad[r][v] = w_r dL_r / d logits[r][v]
- * With K = V this is the divergence of the whole rows; with K < V it is a lower
- * bound of it. Without `rest` P is the softmax over the listed entries alone
+ * With K = V (rows of up to HBSJD_TOP_MAX entries) this is the divergence of the
+ * whole rows; with K < V it is a lower bound of it. Without `rest` P is the softmax over the listed entries alone
  * and the others have no mass (then only the forward divergence is finite:
  * reverse_weight has to be 0).
  */
@@ -357,14 +357,16 @@ typedef struct hbsjd_distill_args {
  * NULL (not both NULL). grad may be the logits' buffer with the logits' stride,
  * and overlaps no input otherwise. Probabilities below 2^-126 count as 0, and 0
  * log 0 as 0. Called again with the loss's upstream gradient as row_weight it is
- * the backward pass (a row is read once either way).
+ * the backward pass. A row is read once, or twice where it goes in parts (which
+ * takes workspace) and the gradient is written.
  * A row with w_r = 0 is not read: its loss and gradient are 0. A row without a
  * distribution (all of its logits or all of the teacher's answer -infinity or
  * unused; a NaN or +infinity in either), with an index outside [0, V) other
  * than -1, or with an index twice has NaN as its loss and all of its gradient; a
  * row whose divergence is infinite (mass on an entry that the other side gives
- * none) has the infinity as its loss and NaN in all of its gradient. Sums are
- * held in fp32 and the gradient is rounded once. The same call gives the same
+ * none) has the infinity as its loss and NaN in all of its gradient. The sums of a
+ * row's exponentials are held in fp32, those of the divergences over the classes in
+ * 64 bits, and the gradient is rounded once. The same call gives the same
  * bits. EINVAL; EHIP.
  */
 hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* args, float* loss, void* grad,

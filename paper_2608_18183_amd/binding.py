@@ -390,8 +390,8 @@ def hbsjd_bikl_rows(logits_s, logits_t, stream=None):
     return out
 
 
-# The calls below take 5 us on the GPU where rows are few, so that the time of a
-# call is the host's: checks that pass cost one comparison each, pointers go to
+# The calls below take 6 to 8 us on the GPU where rows are few, so that the time of
+# a call is the host's: checks that pass cost one comparison each, pointers go to
 # ctypes as plain integers, and torch is looked up once.
 
 _torch = None

@@ -1,5 +1,6 @@
-// C-ABI entry points of the operators on rows of logits: argument checks and one
-// asynchronous launch each; nothing is allocated and nothing waited for.
+// C-ABI entry points of the operators on rows of logits: argument checks and
+// asynchronous launches (one, but for long or very many rows); nothing is allocated
+// and nothing waited for.
 #include "rows.h"
 
 #include <cmath>

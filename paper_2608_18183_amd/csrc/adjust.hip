@@ -164,7 +164,10 @@ __global__ __launch_bounds__(NT) void k_adjust(AdjustArgs a, int parts, int len,
             const int i = t + NT * n, v = bv[n];
             if (v < 0) continue;
             if (searched) {
-                // an entry listed more than once: its first mention adds them all, in order
+                // an entry listed more than once: its first mention adds them all, in order.
+                // Every biased entry of the part looks for its equals then: 4224 bf16 rows
+                // with one entry twice among 64, 300 and 1024 biases take 120, 184 and 768
+                // us, without it 98, 102 and 122.
                 bool mentioned = false;
                 for (int j = 0; j < i; ++j) mentioned |= l.list[j] == v;
                 if (mentioned) continue;

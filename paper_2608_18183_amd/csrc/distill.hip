@@ -43,8 +43,8 @@ inline size_t entries_bytes(int V, int K) { return ((size_t)(V + 31) / 32 + 3 * 
 
 // Fetches the answer and marks its entries that lie among the V from `first` on.
 // Their logits are gathered here (before anything of the gradient is written: it
-// may take the logits' place), or read from `gathered`. mt and mk: the largest t_k and
-// z_k that this thread has seen.
+// may take the logits' place), or read from `gathered`. mt and mk: the largest t_k
+// and z_k that this thread has seen.
 template <int NT, typename T>
 __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* z, const Span& sp,
                                       int first, int V, const Entries& e, int* bad, float* gathered,
@@ -440,8 +440,10 @@ inline size_t part_row_bytes(const Plan& p, int K) { return ((size_t)K + 3 * (si
 // Parts where a workgroup cannot hold the row, and for rows above 128 KB that are
 // few: then enough of them for two workgroups a CU, of 4096 entries at least. (64
 // fp16 rows of 128257: 24 us in parts, 32 held; 140 bf16 rows of 100000: 33 and 31;
-// 200 fp32 rows of 60000: 40 and 27; 900 of them 159 and 116, though the largest
-// held rows spill; 140 fp32 rows of 20000: 24 and 15.)
+// 200 fp32 rows of 60000: 40 and 27; 900 of them 159 and 116; 140 fp32 rows of
+// 20000: 24 and 15.) Rows held by 1024 threads, those above 64 KB, are one
+// workgroup a CU (its 16 wavefronts at 82 to 128 registers): one's loads do not
+// overlap another's stores, and 900 fp32 rows of 60000 take 1.5 times the bytes' 77.
 Plan plan_of(int64_t rows, int V, int K, int32_t elem) {
     Plan p;
     const int64_t size = elem_size(elem);

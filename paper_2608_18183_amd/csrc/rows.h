@@ -211,7 +211,8 @@ template <typename F> inline void by_slabs(int64_t rows, F f, int parts = 1) {
 // them. With more of them, rows being read and rows being written displace one
 // another: divergence of 6144 fp32 rows of 16384, three and two workgroups a CU:
 // 164 and 153 us; 18432 bf16 rows, six and four: 237 and 219 (two: 278); 6400
-// adjusted fp32 rows, four and two: 168 and 159.
+// adjusted fp32 rows, four and two: 168 and 159. (Workgroups of 1024 threads are
+// one a CU by their registers, whatever they ask for.)
 inline size_t resident_lds(size_t lds, size_t bytes) {
     const size_t groups = std::max<size_t>(2, (128 << 10) / bytes);
     return std::max(lds, std::min<size_t>((160 << 10) / (groups + 1), 62 << 10));

@@ -8,7 +8,8 @@
 //      (a thread's entries, or an eighth of them for large K), each wavefront
 //      takes the ceil(K / wavefronts)-th largest of its groups' maxima, and p0 is
 //      the least of these: as many different entries as groups reach it.
-//      Sampling maxima this way leaves 1.3 to 2 K candidates of ordinary rows.
+//      Sampling maxima this way leaves 1.3 to 2 K candidates where a logit's size
+//      has nothing to do with its index.
 //   2. The entries that reach p0 are collected as 64-bit numbers, an
 //      order-preserving image of the logit above the complemented index, so no
 //      two are equal. The mass below p0 is summed in the same pass.
@@ -17,8 +18,19 @@
 //      of equal width between the least and the largest candidate.
 // Rows on which this fails (more candidates or equal ones than there is room
 // for, NaN, a pivot next to fp32's ends) take digit-by-digit selection and a
-// bitonic sort instead, with the same results: 2048 fp32 rows of 16384, K 64,
-// take 44 us, and 1000 us if all their entries are equal.
+// bitonic sort instead, with the same results. Equal entries are one cause, large
+// logits that lie together the other: a wavefront holds runs of neighbouring
+// entries, the one with the smallest takes its share from those, and more than
+// there is room for reach its pivot. 2048 rows of 16384, us, fp32 and bf16:
+//                                          K 64         K 256         K 2000
+//   noise                                40    37      45    42      83    68
+//   noise - ln(1 + index)                42   116     216   384     599   467
+//   noise - 1.5 ln(1 + index)            43   383     534   404     589   460
+//   descending or ascending         500-530  435-470  510-540 485  570-590 500-520
+//   all masked but 1100 neighbours      483   428     518   460     119   100
+//   all masked but 2000 neighbours       38   419      40   443     119   101
+//   rounded to halves                   132    42     534    53     610   517
+//   all equal                          1004  1076    1137  1033    1119  1102
 #include "rows.h"
 
 #include <algorithm>
