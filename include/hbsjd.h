@@ -421,6 +421,167 @@ hbsjd_status hbsjd_adjust_rows(const hbsjd_adjust_args* args, void* out, int32_t
                                int64_t ld_out, void* stream);
 
 /*
+ * Rows of logits and the token that each row's sequence has next: what a policy or
+ * preference step on rollouts takes from them. As the operators above these are
+ * asynchronous, allocate nothing, and take workspace as hbsjd_token_workspace and
+ * hbsjd_preference_workspace say (which are 0 for arguments that would be refused).
+ * With tau the temperature and p = softmax(logits[r] / tau):
+ *   l_r = log p at tokens[r],   H_r = -sum_v p_v log p_v (0 log 0 = 0)
+ * A token of -1 leaves its row out: the row is not read, and its outputs and its
+ * gradient are 0. A row with another token outside [0, V), or without a
+ * distribution (all of its logits -infinity, a NaN or +infinity among them), has NaN
+ * in all outputs and all of its gradient. `grad` (rows of args' elem with stride
+ * ld_grad, or NULL) may be the logits' buffer with the logits' stride, and overlaps
+ * no input otherwise; it is rounded once. Exponentials and their sums are fp32's,
+ * what is made of them is held in 64 bits. The same call gives the same bits.
+ */
+uint64_t hbsjd_token_workspace(int64_t rows, int32_t V, int32_t elem);
+uint64_t hbsjd_preference_workspace(int64_t rows, int32_t V, int32_t elem);
+
+/*
+ * Log-probabilities and entropies, and the gradient of
+ *   sum_r logprob_weight[r] l_r + entropy_weight[r] H_r
+ * by the logits (called with the two outputs' upstream gradients as weights it is
+ * their backward pass).
+ */
+typedef struct hbsjd_logprob_args {
+    int64_t rows;                 /* 0 <= rows < 2^31 */
+    int32_t V;                    /* 1 <= V <= HBSJD_ROWS_MAX_VOCAB */
+    int32_t elem;                 /* hbsjd_elem, of logits and grad */
+    const void* logits;
+    int64_t ld;
+    const int32_t* tokens;        /* [rows], -1: left out */
+    float temperature;            /* in [1e-6, 1e6] */
+    const float* logprob_weight;  /* [rows] or NULL (0) */
+    const float* entropy_weight;  /* [rows] or NULL (0); with grad not both NULL */
+} hbsjd_logprob_args;
+
+/*
+ * logprob, entropy: fp32 [rows] or NULL; not all three outputs NULL. A token whose
+ * logit is -infinity has l = -infinity, and the gradient that its probability of 0
+ * gives. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_logprob_rows(const hbsjd_logprob_args* args, float* logprob, float* entropy,
+                                void* grad, int64_t ld_grad, void* workspace,
+                                uint64_t workspace_bytes, void* stream);
+
+/*
+ * The clipped policy loss with a KL term and an entropy bonus. With A the advantage,
+ * rho = exp(l - old_logprob) and d = ref_logprob - l:
+ *   L_r = -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A)
+ *         + kl_weight (exp(d) - d - 1) - entropy_weight H
+ *   loss[r] = w_r L_r,   grad[r][v] = w_r dL_r / d logits[r][v]
+ * old_logprob, ref_logprob and A are constants to the gradient; the clipped side
+ * passes none, a rho on the bound passes it. Without old_logprob the row's own is
+ * taken (rho = 1, its gradient stays). An A of 0 contributes 0 whatever rho is.
+ */
+typedef struct hbsjd_policy_args {
+    int64_t rows;                 /* 0 <= rows < 2^31 */
+    int32_t V;                    /* 1 <= V <= HBSJD_ROWS_MAX_VOCAB */
+    int32_t elem;                 /* hbsjd_elem, of logits and grad */
+    const void* logits;
+    int64_t ld;
+    const int32_t* tokens;        /* [rows], -1: left out */
+    float temperature;            /* in [1e-6, 1e6] */
+    const float* advantage;       /* [rows] */
+    const float* old_logprob;     /* [rows] or NULL */
+    const float* ref_logprob;     /* [rows] or NULL; not read for kl_weight = 0 */
+    float clip_low;               /* in [0, 1] */
+    float clip_high;              /* in [0, 1e6] */
+    float kl_weight;              /* in [0, 1e6]; > 0 needs ref_logprob */
+    float entropy_weight;         /* in [0, 1e6] */
+    const float* row_weight;      /* [rows] or NULL (1): w_r */
+} hbsjd_policy_args;
+
+/*
+ * loss, logprob (l), entropy: fp32 [rows] or NULL; not all four outputs NULL. A row
+ * with w_r = 0 is left out as one without a token is. A row whose loss is not finite
+ * has it as its loss and NaN in all of its gradient. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_policy_rows(const hbsjd_policy_args* args, float* loss, float* logprob,
+                               float* entropy, void* grad, int64_t ld_grad, void* workspace,
+                               uint64_t workspace_bytes, void* stream);
+
+typedef enum hbsjd_preference_form {
+    HBSJD_PREFERENCE_SIGMOID = 0,  /* -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h) */
+    HBSJD_PREFERENCE_HINGE = 1,    /* max(0, 1 - h) */
+    HBSJD_PREFERENCE_SQUARE = 2    /* (u - 1 / (2 beta))^2 */
+} hbsjd_preference_form;
+
+/*
+ * A preference loss on pairs of sequences: sequence 2 i is the chosen one of pair i,
+ * 2 i + 1 the rejected one. With s the sum of l - ref_logprob over a sequence's rows
+ * that have a token (their mean with `mean`; 0 without any),
+ *   u = s_chosen - s_rejected - margin,   h = beta u,
+ * loss[i] = w_i times the form's value at h or u, and grad its gradient by all rows'
+ * logits. Sequence q has the rows first[q] up to first[q + 1]; rows ahead of the
+ * first sequence and behind the last are left out as rows without a token are.
+ * Without `first` every sequence has rows / (2 pairs) of them.
+ */
+typedef struct hbsjd_preference_args {
+    int64_t rows;                 /* 0 <= rows < 2^31 */
+    int32_t V;                    /* 1 <= V <= HBSJD_ROWS_MAX_VOCAB */
+    int32_t elem;                 /* hbsjd_elem, of logits and grad */
+    const void* logits;
+    int64_t ld;
+    const int32_t* tokens;        /* [rows], -1: left out */
+    float temperature;            /* in [1e-6, 1e6] */
+    int64_t pairs;                /* 0 <= pairs < 2^30 */
+    const int32_t* first;         /* [2 pairs + 1], ascending within [0, rows], or NULL (rows is
+                                     then a multiple of 2 pairs) */
+    const float* ref_logprob;     /* [rows] or NULL (0) */
+    int32_t form;                 /* hbsjd_preference_form */
+    int32_t mean;                 /* 0: sums, else means */
+    float beta;                   /* in [1e-6, 1e6] */
+    float smoothing;              /* in [0, 1); 0 unless the form is the sigmoid's */
+    float margin;                 /* finite */
+    const float* pair_weight;     /* [pairs] or NULL (1): w_i */
+} hbsjd_preference_args;
+
+/*
+ * loss: fp32 [pairs] or NULL; log_ratio: s of every sequence, fp32 [2 pairs] or NULL;
+ * not all three outputs NULL. Rows are read twice where there is a gradient. A pair
+ * with w_i = 0 has the loss 0 and no gradient (its rows are read once, for
+ * log_ratio). A row in error makes its pair's loss NaN. A pair whose loss is not
+ * finite, or whose entries of `first` descend or leave [0, rows], has NaN in the
+ * gradient of its rows that have a token (where the latter makes two pairs claim a
+ * row, either's). EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_preference_rows(const hbsjd_preference_args* args, float* loss, float* log_ratio,
+                                   void* grad, int64_t ld_grad, void* workspace,
+                                   uint64_t workspace_bytes, void* stream);
+
+/*
+ * Lists of tensors, as the gradients of a model's parameters are: the norm of all
+ * entries of all of them, and the tensors scaled so that it does not pass a limit.
+ * Asynchronous as the operators above, with a workspace of
+ * hbsjd_grad_norm_workspace() bytes in any case. The arrays that describe the
+ * tensors are host memory and are not used after the call. Tensor i has sizes[i]
+ * entries (0 <= sizes[i] < 2^40) of type elems[i], one after another from data[i]
+ * on; it may start at any of its elements.
+ *   order 2: the root of the sum of squares, formed in 64 bits; order 0: the largest
+ *   magnitude (either is NaN where an entry is). norm: fp32, one number.
+ */
+#define HBSJD_GRAD_MAX_TENSORS 65536
+uint64_t hbsjd_grad_norm_workspace(void);
+hbsjd_status hbsjd_grad_norm(int64_t count, const void* const* data, const int64_t* sizes,
+                             const int32_t* elems, int32_t order, float* norm, void* workspace,
+                             uint64_t workspace_bytes, void* stream);
+
+/*
+ * As above, and out[i] = data[i] * limit / norm where the norm is above the limit
+ * (the quotient rounded once to fp32, each product once to the tensor's type), else
+ * out[i] = data[i]. `out` NULL: the tensors themselves, which are then not written
+ * unless they are scaled. A norm that is not finite (before it is rounded to fp32)
+ * scales nothing. out[i] is of data[i]'s type and size; written tensors overlap
+ * neither each other nor any other input (EINVAL), out[i] may be data[i]. `norm` is
+ * that of the inputs. limit >= 0, not NaN. EINVAL; EHIP.
+ */
+hbsjd_status hbsjd_clip_grads(int64_t count, void* const* data, const int64_t* sizes,
+                              const int32_t* elems, int32_t order, float limit, void* const* out,
+                              float* norm, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
  * The distribution transform of the verifier rows (Sec. 4.2: the target p and
  * the reused proposals q are full-vocabulary distributions; guided logits under
  * CFG, "Independent progress") on caller-supplied logits, with the draw each

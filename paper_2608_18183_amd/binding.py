@@ -22,6 +22,7 @@ ELEM_F32, ELEM_BF16, ELEM_F16 = 0, 1, 2
 EXEC_AUTO, EXEC_FULL, EXEC_COMPACT = 0, 1, 2
 VERIFY_PROB, VERIFY_GREEDY, VERIFY_AR, VERIFY_AR_GREEDY = 0, 1, 2, 3
 PROGRESS_INDEPENDENT, PROGRESS_SYNC = 0, 1
+_FORMS = {"sigmoid": 0, "hinge": 1, "square": 2}   # hbsjd_preference_form
 KERNELS = ["setup", "embed", "qkv", "attn", "oproj", "norm", "w13", "w2", "lmhead",
            "transform", "verify", "bikl"]
 _WHOLE_ROWS = 16384   # rows of more entries may need a workspace
@@ -73,6 +74,29 @@ class _AdjustArgs(ctypes.Structure):
                 ("mask_row", _P)]
 
 
+class _LogprobArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("V", _I32), ("elem", _I32), ("logits", _P),
+                ("ld", ctypes.c_int64), ("tokens", _P), ("temperature", ctypes.c_float),
+                ("logprob_weight", _P), ("entropy_weight", _P)]
+
+
+class _PolicyArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("V", _I32), ("elem", _I32), ("logits", _P),
+                ("ld", ctypes.c_int64), ("tokens", _P), ("temperature", ctypes.c_float),
+                ("advantage", _P), ("old_logprob", _P), ("ref_logprob", _P),
+                ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float),
+                ("kl_weight", ctypes.c_float), ("entropy_weight", ctypes.c_float),
+                ("row_weight", _P)]
+
+
+class _PreferenceArgs(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("V", _I32), ("elem", _I32), ("logits", _P),
+                ("ld", ctypes.c_int64), ("tokens", _P), ("temperature", ctypes.c_float),
+                ("pairs", ctypes.c_int64), ("first", _P), ("ref_logprob", _P), ("form", _I32),
+                ("mean", _I32), ("beta", ctypes.c_float), ("smoothing", ctypes.c_float),
+                ("margin", ctypes.c_float), ("pair_weight", _P)]
+
+
 _SIGS = {
     "hbsjd_create": (_I32, [ctypes.POINTER(_ModelDesc), ctypes.c_uint64, _P, ctypes.POINTER(_P)]),
     "hbsjd_load_weights": (_I32, [_P, _P, ctypes.c_size_t]),
@@ -90,6 +114,18 @@ _SIGS = {
                                       ctypes.c_uint64, _P]),
     "hbsjd_distill_top_workspace": (ctypes.c_uint64, [ctypes.c_int64, _I32, _I32, _I32]),
     "hbsjd_adjust_rows": (_I32, [ctypes.POINTER(_AdjustArgs), _P, _I32, ctypes.c_int64, _P]),
+    "hbsjd_token_workspace": (ctypes.c_uint64, [ctypes.c_int64, _I32, _I32]),
+    "hbsjd_preference_workspace": (ctypes.c_uint64, [ctypes.c_int64, _I32, _I32]),
+    "hbsjd_logprob_rows": (_I32, [ctypes.POINTER(_LogprobArgs), _P, _P, _P, ctypes.c_int64, _P,
+                                  ctypes.c_uint64, _P]),
+    "hbsjd_policy_rows": (_I32, [ctypes.POINTER(_PolicyArgs), _P, _P, _P, _P, ctypes.c_int64, _P,
+                                 ctypes.c_uint64, _P]),
+    "hbsjd_preference_rows": (_I32, [ctypes.POINTER(_PreferenceArgs), _P, _P, _P, ctypes.c_int64,
+                                     _P, ctypes.c_uint64, _P]),
+    "hbsjd_grad_norm_workspace": (ctypes.c_uint64, []),
+    "hbsjd_grad_norm": (_I32, [ctypes.c_int64, _P, _P, _P, _I32, _P, _P, ctypes.c_uint64, _P]),
+    "hbsjd_clip_grads": (_I32, [ctypes.c_int64, _P, _P, _P, _I32, ctypes.c_float, _P, _P, _P,
+                                ctypes.c_uint64, _P]),
     "hbsjd_verify_probs": (_I32, [_I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "hbsjd_transform_rows": (_I32, [_I32, _I32, _P, _I32, ctypes.c_float, _P, _I32,
                                     ctypes.c_uint64, _P, _P, _P, _P, _P]),
@@ -665,6 +701,276 @@ def hbsjd_adjust_rows(logits, tokens=None, token_count=None, repetition=None, pr
     if given:
         _written(out)
     return out
+
+
+def _gradient(grad, logits):
+    """What a call's `grad` argument asks for: (tensor or None, address, row stride,
+    whether it is the caller's)."""
+    if grad is True:
+        grad = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
+        return grad, grad.data_ptr(), logits.shape[1], False
+    if grad is False or grad is None:
+        return None, None, logits.shape[1], False
+    ld = _matrix(grad, "grad", logits)[2]
+    if grad.dtype is not logits.dtype:
+        raise ValueError("grad: expected the logits' type")
+    return grad, grad.data_ptr(), ld, True
+
+
+def _tokens(t, rows: int, device):
+    if t is None:
+        raise ValueError("tokens: expected a tensor")
+    return _per_row(t, "tokens", rows, _torch.int32, device)
+
+
+def hbsjd_logprob_rows(logits, tokens, temperature: float = 1.0, entropy: bool = False,
+                       logprob_weight=None, entropy_weight=None, grad=None, stream=None):
+    """logits: device tensor [rows, V], fp32, bf16 or fp16, with any row stride;
+    tokens int32 [rows], -1 where a row is left out. Returns (logprob fp32 [rows],
+    entropy fp32 [rows] if asked for, else None, grad like logits or None): grad=True
+    (or a tensor to write, the logits themselves too) is the gradient of
+    sum(logprob_weight * logprob + entropy_weight * entropy), the weights fp32
+    [rows]. Asynchronous on `stream` (the current one by default), as are the calls
+    below. Autograd records none of them; to it, tensors of the caller's that they
+    write are changed in place."""
+    torch = _torch or _load_torch()
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev = _elem(logits.dtype), logits.device
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, tokens, logprob_weight, entropy_weight, grad)):
+            return hbsjd_logprob_rows(logits, tokens, temperature, entropy, logprob_weight,
+                                      entropy_weight, grad)
+    f32 = torch.float32
+    a = _LogprobArgs(rows, V, elem, logits.data_ptr(), ld, _tokens(tokens, rows, dev), temperature,
+                     _per_row(logprob_weight, "logprob_weight", rows, f32, dev),
+                     _per_row(entropy_weight, "entropy_weight", rows, f32, dev))
+    logprob = logits.new_empty((rows,), dtype=f32)
+    entropy = logits.new_empty((rows,), dtype=f32) if entropy else None
+    grad, address, ld_grad, given = _gradient(grad, logits)
+    L = _lib or load_library()
+    ws, nbytes = None, 0
+    if V > _WHOLE_ROWS:
+        nbytes = L.hbsjd_token_workspace(rows, V, elem)
+        ws = logits.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+    st = L.hbsjd_logprob_rows(a, logprob.data_ptr(), None if entropy is None else entropy.data_ptr(),
+                              address, ld_grad, None if ws is None else ws.data_ptr(), nbytes,
+                              torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_logprob_rows")
+    if given:
+        _written(grad)
+    return logprob, entropy, grad
+
+
+def hbsjd_policy_rows(logits, tokens, advantage, old_logprob=None, ref_logprob=None,
+                      temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2,
+                      kl_weight: float = 0.0, entropy_weight: float = 0.0, row_weight=None,
+                      grad=True, entropy=None, stream=None):
+    """The clipped policy loss of rows of logits and its gradient. logits and tokens
+    as for hbsjd_logprob_rows; advantage, old_logprob, ref_logprob and row_weight fp32
+    [rows]. Returns (loss fp32 [rows], grad like logits, logprob fp32 [rows], entropy
+    fp32 [rows]). grad=False leaves the gradient out (None), a tensor is written (the
+    logits themselves too). The entropy is None unless it is part of the loss or asked
+    for."""
+    torch = _torch or _load_torch()
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev = _elem(logits.dtype), logits.device
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, tokens, advantage, old_logprob, ref_logprob,
+                                     row_weight, grad)):
+            return hbsjd_policy_rows(logits, tokens, advantage, old_logprob, ref_logprob,
+                                     temperature, clip_low, clip_high, kl_weight, entropy_weight,
+                                     row_weight, grad, entropy)
+    f32 = torch.float32
+    if advantage is None:
+        raise ValueError("advantage: expected a tensor")
+    a = _PolicyArgs(rows, V, elem, logits.data_ptr(), ld, _tokens(tokens, rows, dev), temperature,
+                    _per_row(advantage, "advantage", rows, f32, dev),
+                    _per_row(old_logprob, "old_logprob", rows, f32, dev),
+                    _per_row(ref_logprob, "ref_logprob", rows, f32, dev), clip_low, clip_high,
+                    kl_weight, entropy_weight, _per_row(row_weight, "row_weight", rows, f32, dev))
+    loss = logits.new_empty((rows,), dtype=f32)
+    logprob = logits.new_empty((rows,), dtype=f32)
+    if entropy is None:
+        entropy = entropy_weight > 0
+    entropy = logits.new_empty((rows,), dtype=f32) if entropy else None
+    grad, address, ld_grad, given = _gradient(grad, logits)
+    L = _lib or load_library()
+    ws, nbytes = None, 0
+    if V > _WHOLE_ROWS:
+        nbytes = L.hbsjd_token_workspace(rows, V, elem)
+        ws = logits.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+    st = L.hbsjd_policy_rows(a, loss.data_ptr(), logprob.data_ptr(),
+                             None if entropy is None else entropy.data_ptr(), address, ld_grad,
+                             None if ws is None else ws.data_ptr(), nbytes,
+                             torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_policy_rows")
+    if given:
+        _written(grad)
+    return loss, grad, logprob, entropy
+
+
+def hbsjd_preference_rows(logits, tokens, first=None, pairs: Optional[int] = None, ref_logprob=None,
+                          temperature: float = 1.0, beta: float = 0.1, form: str = "sigmoid",
+                          mean: bool = False, smoothing: float = 0.0, margin: float = 0.0,
+                          pair_weight=None, grad=True, stream=None):
+    """The preference loss of pairs of sequences and its gradient. logits and tokens as
+    for hbsjd_logprob_rows, sequence after sequence, each pair's chosen one ahead of its
+    rejected one: `pairs` pairs of sequences of one length, or of the rows first[q] up
+    to first[q + 1] (int32 [2 pairs + 1], a device tensor; other rows are left out).
+    ref_logprob fp32 [rows]; form "sigmoid", "hinge" or "square"; pair_weight fp32
+    [pairs]. Returns (loss fp32 [pairs], grad like logits, log_ratio fp32 [2 pairs], the
+    sequences' sums or means of logprob - ref_logprob). grad=False leaves the gradient
+    out (None), a tensor is written (the logits themselves too)."""
+    torch = _torch or _load_torch()
+    rows, V, ld = _matrix(logits, "logits")
+    elem, dev = _elem(logits.dtype), logits.device
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, (logits, tokens, first, ref_logprob, pair_weight, grad)):
+            return hbsjd_preference_rows(logits, tokens, first, pairs, ref_logprob, temperature,
+                                         beta, form, mean, smoothing, margin, pair_weight, grad)
+    f32 = torch.float32
+    if first is not None:
+        if not isinstance(first, torch.Tensor) or first.dim() != 1 or first.numel() % 2 != 1:
+            raise ValueError("first: expected a tensor of shape [2 pairs + 1]")
+        if pairs is not None and pairs != first.numel() // 2:
+            raise ValueError("first and pairs do not go together")
+        pairs = first.numel() // 2
+    elif pairs is None:
+        raise ValueError("need pairs or first")
+    pairs = int(pairs)
+    if not 0 <= pairs <= _INT_MAX:
+        raise ValueError(f"{pairs} pairs")
+    if form not in _FORMS:
+        raise ValueError(f"form: expected one of {', '.join(_FORMS)}")
+    a = _PreferenceArgs(rows, V, elem, logits.data_ptr(), ld, _tokens(tokens, rows, dev),
+                        temperature, pairs,
+                        _per_row(first, "first", 2 * pairs + 1, torch.int32, dev),
+                        _per_row(ref_logprob, "ref_logprob", rows, f32, dev), _FORMS[form],
+                        bool(mean), beta, smoothing, margin,
+                        _per_row(pair_weight, "pair_weight", pairs, f32, dev))
+    loss = logits.new_empty((pairs,), dtype=f32)
+    log_ratio = logits.new_empty((2 * pairs,), dtype=f32)
+    grad, address, ld_grad, given = _gradient(grad, logits)
+    L = _lib or load_library()
+    nbytes = L.hbsjd_preference_workspace(rows, V, elem)
+    ws = logits.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+    st = L.hbsjd_preference_rows(a, loss.data_ptr(), log_ratio.data_ptr(), address, ld_grad,
+                                 None if ws is None else ws.data_ptr(), nbytes,
+                                 torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_preference_rows")
+    if given:
+        _written(grad)
+    return loss, grad, log_ratio
+
+
+def _order(order) -> int:
+    if order == 2:
+        return 2
+    if order == float("inf"):
+        return 0
+    raise ValueError("order: expected 2 or infinity")
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's entries lie one after another, in some order."""
+    if t.is_contiguous():
+        return True
+    n = 1
+    for stride, size in sorted((s, k) for s, k in zip(t.stride(), t.shape) if k != 1):
+        if stride != n:
+            return False
+        n *= size
+    return True
+
+
+def _described(tensors, what: str, device):
+    """The addresses, sizes and types of dense device tensors, as arrays for C."""
+    types = _ELEMS
+    for t in tensors:
+        if not isinstance(t, _torch.Tensor) or t.device != device or t.layout is not _torch.strided:
+            raise ValueError(f"{what}: expected tensors on {device}")
+        if t.dtype not in types:
+            raise ValueError(f"{what}: fp32, bf16 or fp16, not {t.dtype}")
+        if not t.is_contiguous() and not _dense(t):
+            raise ValueError(f"{what}: a tensor's entries have to lie one after another")
+    n = len(tensors)
+    return ((_P * n)(*[t.data_ptr() for t in tensors]),
+            (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
+            (_I32 * n)(*[types[t.dtype] for t in tensors]))
+
+
+def _list_device(tensors):
+    """The device of a list of tensors; the current one of an empty list."""
+    torch = _torch
+    if not tensors:
+        return torch.device("cuda", torch.cuda.current_device())
+    t = tensors[0]
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("grads: expected device tensors")
+    return t.device
+
+
+def hbsjd_grad_norm(grads, order: float = 2.0, stream=None):
+    """The norm of all entries of a list of device tensors (fp32, bf16 or fp16, mixed
+    as they come, each with its entries one after another): the root of the sum of
+    squares, or with order=inf the largest magnitude. Returns a device tensor fp32 []."""
+    torch = _torch or _load_torch()
+    grads = list(grads)
+    dev = _list_device(grads)
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, grads):
+            return hbsjd_grad_norm(grads, order)
+    order = _order(order)
+    data, sizes, elems = _described(grads, "grads", dev)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    L = _lib or load_library()
+    nbytes = L.hbsjd_grad_norm_workspace()
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+    st = L.hbsjd_grad_norm(len(grads), data, sizes, elems, order, norm.data_ptr(), ws.data_ptr(),
+                           nbytes, torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_grad_norm")
+    return norm
+
+
+def hbsjd_clip_grads(grads, limit: float, order: float = 2.0, out=None, stream=None):
+    """Scales a list of device tensors (as hbsjd_grad_norm takes them) by limit / norm
+    where their norm is above the limit. In place, or into the tensors of the list
+    `out`, of the same shapes, types and strides (copies where nothing is scaled).
+    Returns the norm ahead of the scaling, a device tensor fp32 []. A norm that is not
+    finite scales nothing."""
+    torch = _torch or _load_torch()
+    grads = list(grads)
+    dev = _list_device(grads)
+    out = None if out is None else list(out)
+    if not _here(dev, stream):
+        with _OnStream(dev, stream, grads + (out or [])):
+            return hbsjd_clip_grads(grads, limit, order, out)
+    order = _order(order)
+    data, sizes, elems = _described(grads, "grads", dev)
+    out_at = None
+    if out is not None:
+        if len(out) != len(grads):
+            raise ValueError(f"out: expected {len(grads)} tensors")
+        for g, o in zip(grads, out):
+            if (not isinstance(o, torch.Tensor) or o.dtype is not g.dtype or o.shape != g.shape
+                    or o.device != dev or o.stride() != g.stride()):
+                raise ValueError("out: expected tensors of the same shapes, types and strides")
+        out_at = (_P * len(out))(*[o.data_ptr() for o in out])
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    L = _lib or load_library()
+    nbytes = L.hbsjd_grad_norm_workspace()
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
+    st = L.hbsjd_clip_grads(len(grads), data, sizes, elems, order, limit, out_at, norm.data_ptr(),
+                            ws.data_ptr(), nbytes, torch._C._cuda_getCurrentRawStream(dev.index))
+    if st:
+        _check(st, "hbsjd_clip_grads")
+    if grads:
+        _written(*(grads if out is None else out))
+    return norm
 
 
 def hbsjd_mfma_probe(workgroups: int, iters: int, sink, stream=None):

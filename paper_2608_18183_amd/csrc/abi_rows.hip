@@ -1,49 +1,9 @@
 // C-ABI entry points of the operators on rows of logits: argument checks and
 // asynchronous launches (one, but for long or very many rows); nothing is allocated
 // and nothing waited for.
-#include "rows.h"
-
-#include <cmath>
+#include "abi_checks.h"
 
 using namespace hbsjd;
-
-namespace {
-
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
-
-bool elem_ok(int32_t e) { return e == HBSJD_ELEM_F32 || e == HBSJD_ELEM_BF16 || e == HBSJD_ELEM_F16; }
-bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
-
-// null, or why a [rows][V] matrix cannot be taken
-const char* matrix_problem(const void* p, int32_t elem, int64_t ld, int32_t V) {
-    if (!elem_ok(elem)) return "unknown element type";
-    if (!p) return "NULL buffer";
-    if (!aligned(p, elem_size(elem))) return "buffer not aligned to its elements";
-    if (ld < V || ld > kMaxStride) return "row stride below V or above 2^40";
-    return nullptr;
-}
-
-const char* rows_problem(int64_t rows, int32_t V) {
-    if (rows < 0 || rows > INT32_MAX) return "need 0 <= rows < 2^31";
-    if (V < 1 || V > HBSJD_ROWS_MAX_VOCAB) return "need V in [1, 262144]";
-    return nullptr;
-}
-
-const char* workspace_problem(const void* p, uint64_t bytes, uint64_t need) {
-    if (need && (!p || bytes < need)) return "workspace smaller than the call needs";
-    if (need && !aligned(p, 16)) return "workspace not aligned to 16 bytes";
-    return nullptr;
-}
-
-bool temperature_ok(float t) { return t >= 1e-6f && t <= 1e6f; }
-
-hbsjd_status launched(const char* where) {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return api_fail(HBSJD_EHIP, std::string(where) + ": " + hipGetErrorString(e));
-    return HBSJD_OK;
-}
-
-}  // namespace
 
 extern "C" {
 
@@ -118,12 +78,8 @@ hbsjd_status hbsjd_distill_top_rows(const hbsjd_distill_args* p, float* loss, vo
         if (const char* why = workspace_problem(
                 workspace, workspace_bytes, distill_top_workspace(p->rows, p->V, p->K, p->elem)))
             return api_fail(HBSJD_EINVAL, why);
-        const double log2_tau = 1.4426950408889634074 / (double)p->temperature;
-        float log2_hi = (float)log2_tau;   // rounded down: the rest is positive
-        if ((double)log2_hi >= log2_tau) log2_hi = std::nextafterf(log2_hi, 0.f);
-        const float log2_lo = (float)(log2_tau - (double)log2_hi);
         DistillArgs a{p->rows, p->V, p->K, p->logits, p->elem, p->ld, p->values, p->index, p->rest,
-                      1.f / p->temperature, 1.0 / p->temperature, make_float2(log2_hi, log2_lo),
+                      1.f / p->temperature, 1.0 / p->temperature, log2_over(p->temperature),
                       alpha, beta, p->row_weight, loss, grad, ld_grad};
         distill_top(a, workspace, (hipStream_t)stream);
         return launched("distill_top_rows");

@@ -20,9 +20,6 @@
 namespace hbsjd {
 namespace {
 
-constexpr float kNan = __builtin_nanf("");
-constexpr float kLn2 = 0.6931471805599453f;
-
 // What a workgroup of NT threads works out about a row once the row's unlisted
 // maximum is known; the same for every way the row itself is held.
 struct Entries {
@@ -78,15 +75,6 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int64_t r, const T* 
         e.entry[k] = v;
         e.tk[k] = x;
     }
-}
-
-// exp of a number held in 64 bits, to a rounding or two of fp32: the hardware's
-// exp2 takes 32 bits, the argument's own rounding is put back to first order
-__device__ __forceinline__ float exp_of(double x) {
-    const double u = x * 1.4426950408889634074;
-    const float h = (float)u;
-    const float e = __builtin_amdgcn_exp2f(h);
-    return h < -200.f ? 0.f : fmaf(e, (float)(u - (double)h) * kLn2, e);
 }
 
 struct RowStats {
@@ -186,43 +174,14 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Entr
     }
 }
 
-// a gradient row of one value
-template <int NT, typename T>
-__device__ __forceinline__ void fill_row(T* g, int V, float x) {
-    const Span sp = Span::of(g, V);
-    float xs[kVec<T>];
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) xs[i] = x;
-    const u32x4 raw = vec_pack<T>(xs);
-    u32x4* g4 = (u32x4*)(g + sp.head);
-    for (int j = threadIdx.x; j < sp.vecs; j += NT) g4[j] = raw;
-    if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(x);
-}
-
-// exp(d / tau): log2 e / tau in two parts, since the rounding of one alone would
-// put all entries of the sum off the same way. (Both are positive: d = -infinity
-// gives 0.)
-__device__ __forceinline__ float power(float d, float2 c2) {
-    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
-}
-
 // ---- a row, or a part of one, in registers: NV 16-byte vectors a thread
 
-template <typename T, int NT, int NV> struct Held {
-    static constexpr int E = kVec<T>;
-    u32x4 x[NV];
-    float xe;   // this thread's edge entry
-    Span sp;
+template <typename T, int NT, int NV> struct Held : RowRegs<T, NT, NV> {
+    using RowRegs<T, NT, NV>::E;
+    using RowRegs<T, NT, NV>::x;
+    using RowRegs<T, NT, NV>::xe;
+    using RowRegs<T, NT, NV>::sp;
 
-    __device__ __forceinline__ void load(const T* z, int V) {
-        sp = Span::of(z, V);
-        xe = -INFINITY;
-        const u32x4* z4 = (const u32x4*)(z + sp.head);
-        if (sp.vecs > 0)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min((int)threadIdx.x + NT * i, sp.vecs - 1));
-        if ((int)threadIdx.x < sp.edges()) xe = widen(z[sp.edge(threadIdx.x, V)]);
-    }
     // Listed entries become -infinity, so that the maximum, the sum and the
     // gradient's factor are of the unlisted ones alone. Returns the largest.
     __device__ __forceinline__ float mask(const uint32_t* listed) {
@@ -292,8 +251,6 @@ template <typename T, int NT, int NV> struct Held {
         if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(f * xe);
     }
 };
-
-constexpr int waves_of(int nt) { return nt == 1024 ? 4 : 5; }
 
 // A workgroup of NT threads per row: logits leave memory once. The gradient at
 // the listed entries is stored over the row's afterwards.

@@ -1,6 +1,7 @@
 // Operators on rows of logits that stand on their own (a teacher's top logits,
-// the divergence from them with its gradient, penalties, biases and masks):
-// what their kernels share, and the host launchers (internal interface).
+// the divergence from them with its gradient, penalties, biases and masks, tokens'
+// log-probabilities, policy and preference losses): what their kernels share, and
+// the host launchers (internal interface).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -195,6 +196,62 @@ template <int NT, typename F> __device__ __forceinline__ float block_all(float v
     return a[0];
 }
 
+// ------------------------------------------------------------ exponentials
+constexpr float kNan = __builtin_nanf("");
+constexpr float kLn2 = 0.6931471805599453f;
+
+// exp of a number held in 64 bits, to a rounding or two of fp32: the hardware's
+// exp2 takes 32 bits, the argument's own rounding is put back to first order
+__device__ __forceinline__ float exp_of(double x) {
+    const double u = x * 1.4426950408889634074;
+    const float h = (float)u;
+    const float e = __builtin_amdgcn_exp2f(h);
+    return h < -200.f ? 0.f : fmaf(e, (float)(u - (double)h) * kLn2, e);
+}
+
+// exp(d / tau): log2 e / tau in two parts, since the rounding of one alone would
+// put all entries of the sum off the same way. (Both are positive: d = -infinity
+// gives 0.)
+__device__ __forceinline__ float power(float d, float2 c2) {
+    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
+}
+
+// ------------------------------------------------------------ rows in registers
+// a row of one value
+template <int NT, typename T>
+__device__ __forceinline__ void fill_row(T* g, int V, float x) {
+    const Span sp = Span::of(g, V);
+    float xs[kVec<T>];
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) xs[i] = x;
+    const u32x4 raw = vec_pack<T>(xs);
+    u32x4* g4 = (u32x4*)(g + sp.head);
+    for (int j = threadIdx.x; j < sp.vecs; j += NT) g4[j] = raw;
+    if ((int)threadIdx.x < sp.edges()) g[sp.edge(threadIdx.x, V)] = narrow<T>(x);
+}
+
+// A row, or a part of one, held by a workgroup of NT threads: NV 16-byte vectors
+// a thread (those behind the row's end repeat its last) and an edge entry.
+template <typename T, int NT, int NV> struct RowRegs {
+    static constexpr int E = kVec<T>;
+    u32x4 x[NV];
+    float xe;   // this thread's edge entry
+    Span sp;
+
+    __device__ __forceinline__ void load(const T* z, int V) {
+        sp = Span::of(z, V);
+        xe = -INFINITY;
+        const u32x4* z4 = (const u32x4*)(z + sp.head);
+        if (sp.vecs > 0)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) x[i] = vec_at(z4, min((int)threadIdx.x + NT * i, sp.vecs - 1));
+        if ((int)threadIdx.x < sp.edges()) xe = widen(z[sp.edge(threadIdx.x, V)]);
+    }
+};
+
+// wavefronts a SIMD that the registers of such kernels leave room for
+constexpr int waves_of(int nt) { return nt == 1024 ? 4 : 5; }
+
 // Launches over slabs of rows: one launch of all rows could pass the 2^32 work
 // items that a launch may have. (Workgroups that loop over rows hold whatever
 // the compiler moves out of the loop: 96 registers and spills in place of 81 in
@@ -279,5 +336,50 @@ struct AdjustArgs {
     const int32_t* mask_row;     // [rows] or null
 };
 void adjust_rows(const AdjustArgs& a, hipStream_t s);
+
+// Rows of logits and a token of each: the log-probability l, the entropy H, a
+// loss of them (its own or a pair's) and the loss's gradient.
+struct TokenArgs {
+    int64_t rows;
+    int V;
+    const void* logits;
+    int32_t elem;
+    int64_t ld;
+    const int32_t* tokens;         // [rows], -1: the row takes no part
+    double inv_tau;
+    float2 log2_tau;               // log2 e / temperature in two parts
+    void* grad;                    // [rows], stride ld_grad, or null
+    int64_t ld_grad;
+    float* logprob;                // [rows] or null
+    float* entropy;                // [rows] or null
+    // the loss is a sum of l and H with these weights...
+    const float* logprob_weight;   // [rows] or null: 0
+    const float* entropy_weight;   // [rows] or null: 0
+    // ...or, with advantages, the clipped policy loss
+    const float* advantage;        // [rows] or null
+    const float* old_logprob;      // [rows] or null: the row's own
+    const float* ref_logprob;      // [rows] or null
+    double low, high;              // bounds of the ratio
+    float kl, bonus;
+    const float* weight;           // [rows] or null: 1
+    float* loss;                   // [rows] or null
+};
+// bytes of workspace that a call needs
+size_t token_workspace(int64_t rows, int V, int32_t elem);
+void token_rows(const TokenArgs& a, void* workspace, hipStream_t s);
+
+struct PreferenceArgs {
+    int64_t pairs;
+    const int32_t* first;          // [2 pairs + 1], or null: sequences of rows / (2 pairs)
+    const float* ref_logprob;      // [rows] or null: 0
+    int32_t form;                  // hbsjd_preference_form
+    bool mean;
+    double beta, smoothing, margin;
+    const float* weight;           // [pairs] or null: 1
+    float* loss;                   // [pairs] or null
+    float* log_ratio;              // [2 pairs] or null
+};
+size_t preference_workspace(int64_t rows, int V, int32_t elem);
+void preference_rows(const TokenArgs& a, const PreferenceArgs& p, void* workspace, hipStream_t s);
 
 }  // namespace hbsjd

@@ -1,0 +1,649 @@
+// Log-probabilities of rows' tokens, the losses made of them, and their gradients
+// by the logits.
+//
+// With p = softmax(z / tau) of a row, y its token, l = log p_y and H = -sum p log p:
+//   dl/dz_v = (1[v = y] - p_v) / tau,   dH/dz_v = -p_v (log p_v + H) / tau.
+// All losses here reach the logits through the two slopes g = dL/dl and h = dL/dH.
+// With m the row's largest logit, d_v = z_v - m, e_v = exp(d_v / tau), s = sum e
+// and T = sum e d, H - log s = -T / (tau s), and the gradient is
+//   e_v (A_0 + A_1 d_v),   A_0 = -(g - h T / (tau s)) / (tau s),   A_1 = -h / (tau^2 s)
+// away from the token, and at it
+//   (g s_o / s - h e_y (d_y - T / s) / (tau s)) / tau,
+// s_o the sum over all entries but the token's. That sum is formed by itself: for a
+// token that is nearly certain, 1 - p_y = s_o / s and l = -log(1 + s_o / e_y) would
+// be differences of almost equal numbers.
+//
+// A row is read once and stays in its workgroup's registers until its gradient is
+// stored; long rows go in parts, pairs of sequences in two readings with the pair's
+// loss between them.
+#include "rows.h"
+
+#include <algorithm>
+
+namespace hbsjd {
+namespace {
+
+// exponents (to base 2) below this give an e_v of 0 in any case
+constexpr float kFar = -200.f;
+
+// What the entries of a row or a part come to.
+struct Sums {
+    double s = 0.0, t = 0.0;   // without the token's entry
+};
+
+template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
+    using RowRegs<T, NT, NV>::E;
+    using RowRegs<T, NT, NV>::x;
+    using RowRegs<T, NT, NV>::xe;
+    using RowRegs<T, NT, NV>::sp;
+    int jy, qy, ey;   // the token's vector and place in it, or its edge; -1: elsewhere
+
+    // y: the token's entry relative to this row or part
+    __device__ __forceinline__ void find(int y, int V) {
+        jy = ey = -1;
+        qy = 0;
+        if (y < 0 || y >= V) return;
+        const int p = sp.place(y, V);
+        if (p >= sp.vecs * E) {
+            ey = p - sp.vecs * E;
+        } else {
+            jy = p / E;
+            qy = p % E;
+        }
+    }
+    // The token's entry and what lies behind the row become -infinity. Returns the
+    // largest of the rest.
+    __device__ __forceinline__ float largest() {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = threadIdx.x + NT * i;
+            if (j >= sp.vecs) {
+                x[i] = masked_vec<T>();
+                continue;
+            }
+            if (j == jy)
+#pragma unroll
+                for (int q = 0; q < E; ++q) vec_mask<T>(x[i], q, q == qy);
+#pragma unroll
+            for (int q = 0; q < E; ++q) m = fmaxf(m, vec_get<T>(x[i], q));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if ((int)threadIdx.x == ey) xe = -INFINITY;
+        return fmaxf(m, xe);
+    }
+    template <bool Ent>
+    __device__ __forceinline__ void add(float d, float2 c2, float far, float& s, float& t) {
+        const float e = power(d, c2);
+        s += e;
+        if constexpr (Ent) t = fmaf(e, fmaxf(d, far), t);
+    }
+    // this thread's part of s and T
+    template <bool Ent> __device__ __forceinline__ Sums sum(float m, float2 c2, float far) {
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float sv = 0.f, tv = 0.f;   // a vector's own sums: shorter chains of roundings
+#pragma unroll
+            for (int q = 0; q < E; ++q) add<Ent>(vec_get<T>(x[i], q) - m, c2, far, sv, tv);
+            s += sv;
+            t += tv;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        add<Ent>(xe - m, c2, far, s, t);
+        return Sums{(double)s, (double)t};
+    }
+    template <bool Ent>
+    __device__ __forceinline__ static float value(float d, float2 c2, float far, float a0, float a1) {
+        // 16-bit gradients: what log2 e / tau loses as one number lies below their rounding
+        const float e = E == 4 ? power(d, c2) : __builtin_amdgcn_exp2f(d * c2.x);
+        return Ent ? e * fmaf(a1, fmaxf(d, far), a0) : e * a0;
+    }
+    // the gradient, after largest(); gy: at the token
+    template <bool Ent>
+    __device__ __forceinline__ void store(T* g, const T* z, int V, float m, float2 c2, float far, float a0,
+                                          float a1, float gy) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
+        const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
+        T* gv = g + sp.head;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int j = threadIdx.x + NT * i;
+            float y[E];
+#pragma unroll
+            for (int q = 0; q < E; ++q) y[q] = value<Ent>(vec_get<T>(x[i], q) - m, c2, far, a0, a1);
+            if (j == jy)
+#pragma unroll
+                for (int q = 0; q < E; ++q) y[q] = q == qy ? gy : y[q];
+            __builtin_amdgcn_sched_barrier(0);
+            if (j >= sp.vecs) continue;
+            if (same) {
+                vec_at((u32x4*)gv, j) = vec_pack<T>(y);
+            } else {
+#pragma unroll
+                for (int q = 0; q < E; ++q) gv[j * E + q] = narrow<T>(y[q]);
+            }
+        }
+        if ((int)threadIdx.x < sp.edges()) {
+            const float ye = value<Ent>(xe - m, c2, far, a0, a1);
+            g[sp.edge(threadIdx.x, V)] = narrow<T>((int)threadIdx.x == ey ? gy : ye);
+        }
+    }
+};
+
+// ---- a row's results from its sums
+
+struct RowEnd {
+    double l, entropy, s, se, t;   // s: all of the row; se: without the token; t: all
+    double ey, dy;
+};
+
+// m: the largest logit, zy: the token's
+__device__ __forceinline__ RowEnd row_end(float m, float zy, Sums o, double inv_tau) {
+    RowEnd r;
+    r.dy = (double)zy - (double)m;
+    const double x = r.dy * inv_tau;
+    r.ey = exp_of(x);
+    r.se = o.s;
+    r.s = o.s + r.ey;
+    r.t = r.ey > 0.0 ? o.t + r.ey * r.dy : o.t;
+    r.l = r.ey >= o.s ? -log1p(o.s / r.ey) : x - log(r.s);
+    r.entropy = (r.ey >= o.s ? x - r.l : log(r.s)) - r.t * inv_tau / r.s;
+    // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or NaN)
+    if (!(r.s > 0.0 && r.s < INFINITY)) r.l = r.entropy = (double)kNan;
+    return r;
+}
+
+struct Goal {
+    double loss, g, h;
+};
+
+// The loss of row r and its slopes by l and H, w the row's weight.
+__device__ __forceinline__ Goal goal_of(const TokenArgs& a, int64_t r, double l, double entropy, float w) {
+    Goal o{0.0, 0.0, 0.0};
+    if (!a.advantage) {
+        if (a.logprob_weight) o.g = a.logprob_weight[r];
+        if (a.entropy_weight) o.h = a.entropy_weight[r];
+        o.loss = l;   // whose being no number the gradient shows
+        return o;
+    }
+    const double adv = a.advantage[r];
+    const double rho = a.old_logprob ? exp(l - (double)a.old_logprob[r]) : l == l ? 1.0 : l;
+    const double bound = adv > 0.0 ? a.high : a.low;
+    const bool beyond = adv > 0.0 ? rho > bound : rho < bound;
+    if (adv != 0.0) {   // (a NaN is taken along)
+        o.loss = -adv * (beyond ? bound : rho);
+        o.g = beyond ? 0.0 : -adv * rho;
+    } else if (rho != rho) {
+        o.loss = rho;
+    }
+    if (a.kl > 0.f && a.ref_logprob) {
+        const double d = (double)a.ref_logprob[r] - l, e = expm1(d);
+        o.loss += a.kl * (e < INFINITY ? e - d : e);
+        o.g -= a.kl * e;
+    }
+    if (a.bonus > 0.f) {
+        o.loss -= a.bonus * entropy;
+        o.h = -a.bonus;
+    }
+    o.loss *= w;
+    o.g *= w;
+    o.h *= w;
+    return o;
+}
+
+// what the stores need
+struct Slopes {
+    float a0, a1, gy;
+    bool ok;
+};
+__device__ __forceinline__ Slopes slopes_of(const RowEnd& e, const Goal& o, double inv_tau) {
+    const double f = inv_tau / e.s, mean = e.t / e.s;   // of d
+    Slopes s;
+    s.a0 = (float)(-f * (o.g - o.h * mean * inv_tau));
+    s.a1 = (float)(-f * o.h * inv_tau);
+    const double py_d = e.ey > 0.0 ? e.ey * (e.dy - mean) : 0.0;
+    s.gy = (float)(f * (o.g * e.se - o.h * py_d * inv_tau));
+    return s;
+}
+
+// a row that takes no part
+template <int NT, typename T>
+__device__ __forceinline__ void no_part(const TokenArgs& a, int64_t r, T* g, int V, bool first) {
+    if (g) fill_row<NT>(g, V, 0.f);
+    if (first && threadIdx.x == 0) {
+        if (a.loss) a.loss[r] = 0.f;
+        if (a.logprob) a.logprob[r] = 0.f;
+        if (a.entropy) a.entropy[r] = 0.f;
+    }
+}
+template <int NT, typename T>
+__device__ __forceinline__ void no_number(const TokenArgs& a, int64_t r, T* g, int V, bool first) {
+    if (g) fill_row<NT>(g, V, kNan);
+    if (first && threadIdx.x == 0) {
+        if (a.loss) a.loss[r] = kNan;
+        if (a.logprob) a.logprob[r] = kNan;
+        if (a.entropy) a.entropy[r] = kNan;
+    }
+}
+
+// One wavefront works a row out in 64 bits and leaves the slopes in `shared`
+// (every wavefront doing so would take as long as the exponentials).
+__device__ __forceinline__ void finish(const TokenArgs& a, int64_t r, float m, float zy, Sums o, float w,
+                                       bool first, Slopes* shared) {
+    const RowEnd e = row_end(m, zy, o, a.inv_tau);
+    const Goal goal = goal_of(a, r, e.l, e.entropy, w);
+    Slopes s = slopes_of(e, goal, a.inv_tau);
+    // a loss without an end leaves no gradient; a log-probability of -infinity does
+    const float loss = (float)goal.loss;
+    s.ok = a.advantage ? loss > -INFINITY && loss < INFINITY : loss == loss;
+    if (threadIdx.x == 0) {
+        *shared = s;
+        if (first) {
+            if (a.loss) a.loss[r] = loss;
+            if (a.logprob) a.logprob[r] = (float)e.l;
+            if (a.entropy) a.entropy[r] = (float)e.entropy;
+        }
+    }
+}
+
+__device__ __forceinline__ float far_of(const TokenArgs& a) { return kFar / a.log2_tau.x; }
+
+// A workgroup of NT threads a row.
+template <typename T, int NT, int NV, bool Ent>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_token(
+    TokenArgs a, int64_t r0) {
+    __shared__ float red[NT / 64];
+    __shared__ double red2[2][NT / 64];
+    __shared__ Slopes shared;
+    const int64_t r = r0 + blockIdx.x;
+    const T* z = (const T*)a.logits + r * a.ld;
+    T* g = a.grad ? (T*)a.grad + r * a.ld_grad : nullptr;
+    const int y = a.tokens[r];
+    const float w = a.weight ? a.weight[r] : 1.f;
+    if (y == -1 || w == 0.f) return no_part<NT>(a, r, g, a.V, true);
+    if (y < 0 || y >= a.V) return no_number<NT>(a, r, g, a.V, true);
+    TokenRow<T, NT, NV> row;
+    row.load(z, a.V);
+    const float zy = widen(z[y]);
+    row.find(y, a.V);
+    float m = block_all<NT>(row.largest(), red, MaxOp());
+    m = fmaxf(m, zy);
+    const float2 c2 = a.log2_tau;
+    const float far = far_of(a);
+    const Sums o = row.template sum<Ent>(m, c2, far);
+    double s[2] = {o.s, o.t};
+    block_all<NT, Ent ? 2 : 1>(*(double(*)[Ent ? 2 : 1])s, red2, AddOp());
+    if (threadIdx.x < 64) finish(a, r, m, zy, Sums{s[0], s[1]}, w, true, &shared);
+    if (!g) return;
+    __syncthreads();
+    const Slopes sl = shared;
+    if (!sl.ok) return fill_row<NT>(g, a.V, kNan);
+    row.template store<Ent>(g, z, a.V, m, c2, far, uniform(sl.a0), uniform(sl.a1), uniform(sl.gy));
+}
+
+// ---- rows in parts
+
+// what a part leaves in the workspace
+struct PartStats {
+    float m, s, t, zy;   // zy: the token's logit, in the part that holds it
+};
+struct PartsArgs {
+    int parts, len;
+    PartStats* stats;   // [rows][parts]
+};
+
+// the sums of a part, or of a whole row where parts = 1
+template <typename T, int NT, int NV, bool Ent>
+__device__ __forceinline__ void part_stats(const TokenArgs& a, const PartsArgs& p, int64_t r, int c, int y,
+                                           PartStats* out) {
+    __shared__ float red[NT / 64];
+    __shared__ double red2[2][NT / 64];
+    const int first = c * p.len, V = min(p.len, a.V - first);
+    const T* z = (const T*)a.logits + r * a.ld + first;
+    TokenRow<T, NT, NV> row;
+    row.load(z, V);
+    const bool here = y >= first && y < first + V;
+    const float zy = here ? widen(z[y - first]) : 0.f;
+    row.find(y - first, V);
+    const float m = block_all<NT>(row.largest(), red, MaxOp());
+    // relative to a finite number: a part of -infinities sums to 0
+    const Sums o = row.template sum<Ent>(m == -INFINITY ? 0.f : m, a.log2_tau, far_of(a));
+    double s[2] = {o.s, o.t};
+    block_all<NT, Ent ? 2 : 1>(*(double(*)[Ent ? 2 : 1])s, red2, AddOp());
+    if (threadIdx.x == 0) *out = PartStats{m, (float)s[0], Ent ? (float)s[1] : 0.f, zy};
+}
+
+// The sums of a part relative to the row's largest logit.
+template <bool Ent>
+__device__ __forceinline__ Sums part_sums(const PartStats& q, float m, float2 c2, float far) {
+    if (q.m == -INFINITY) return Sums{(double)q.s, 0.0};
+    const float d = q.m - m, e = power(d, c2);
+    return Sums{(double)q.s * e, Ent ? ((double)q.t + (double)q.s * fmaxf(d, far)) * e : 0.0};
+}
+
+template <typename T, int NT, int NV, bool Ent>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_token_part(
+    TokenArgs a, PartsArgs p, int64_t r0) {
+    const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
+    const int64_t r = r0 + row;
+    const int y = a.tokens[r];
+    if (y < 0 || y >= a.V || (a.weight && a.weight[r] == 0.f)) return;
+    part_stats<T, NT, NV, Ent>(a, p, r, c, y, p.stats + (int64_t)row * p.parts + c);
+}
+
+// Joins a row's parts (every part's workgroup does, a lane a part) and stores the
+// gradient, reading the part again.
+template <typename T, int NT, int NV, bool Ent>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_token_rest(
+    TokenArgs a, PartsArgs p, int64_t r0) {
+    __shared__ Slopes shared;
+    const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
+    const int64_t r = r0 + row;
+    const int first = c * p.len, V = min(p.len, a.V - first);
+    const T* z = (const T*)a.logits + r * a.ld + first;
+    T* g = a.grad ? (T*)a.grad + r * a.ld_grad + first : nullptr;
+    const int y = a.tokens[r];
+    const float w = a.weight ? a.weight[r] : 1.f;
+    if (y == -1 || w == 0.f) return no_part<NT>(a, r, g, V, c == 0);
+    if (y < 0 || y >= a.V) return no_number<NT>(a, r, g, V, c == 0);
+    TokenRow<T, NT, NV> part;
+    if (g) part.load(z, V);
+    else if (c > 0) return;   // without a gradient one workgroup a row is enough
+    const PartStats* stats = p.stats + (int64_t)row * p.parts;
+    const int lane = threadIdx.x & 63;
+    const float2 c2 = a.log2_tau;
+    const float far = far_of(a), zy = stats[y / p.len].zy;
+    PartStats q{-INFINITY, 0.f, 0.f, 0.f};
+    if (lane < p.parts) q = stats[lane];
+    const float m = fmaxf(wave_all(q.m, MaxOp()), zy);
+    if (threadIdx.x < 64) {
+        Sums o = part_sums<Ent>(q, m, c2, far);
+        o.s = wave_all(o.s, AddOp());
+        if constexpr (Ent) o.t = wave_all(o.t, AddOp());
+        finish(a, r, m, zy, o, w, c == 0, &shared);
+    }
+    if (!g) return;
+    __syncthreads();
+    const Slopes sl = shared;
+    if (!sl.ok) return fill_row<NT>(g, V, kNan);
+    part.find(y - first, V);
+    part.largest();
+    part.template store<Ent>(g, z, V, m, c2, far, uniform(sl.a0), uniform(sl.a1), uniform(sl.gy));
+}
+
+// ---- pairs of sequences
+
+// what the pair leaves for a row
+struct RowSlope {
+    float m, a0, gy;
+    int used;
+};
+struct PairArgs {
+    PartsArgs p;
+    RowSlope* slope;   // [rows]
+};
+
+// the first reading: a row's sums
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_pair_stats(
+    TokenArgs a, PreferenceArgs q, PairArgs b, int64_t r0) {
+    const int row = blockIdx.x / b.p.parts, c = blockIdx.x - row * b.p.parts;
+    const int64_t r = r0 + row;
+    const int y = a.tokens[r];
+    // rows ahead of the first sequence and behind the last are left out
+    const bool in = !q.first || (r >= q.first[0] && r < q.first[2 * q.pairs]);
+    if (c == 0 && threadIdx.x == 0) b.slope[r] = RowSlope{0.f, 0.f, 0.f, 0};
+    if (!in || y < 0 || y >= a.V) return;
+    part_stats<T, NT, NV, false>(a, b.p, r, c, y, b.p.stats + r * b.p.parts + c);
+}
+
+constexpr int kPairThreads = 1024;
+
+__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+__device__ __forceinline__ double logistic(double x) { return 1.0 / (1.0 + exp(-x)); }
+
+// A workgroup a pair: its rows' log-probabilities, its loss, and the slope that
+// each of its rows takes from that.
+__global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceArgs q, PairArgs b,
+                                                       int64_t pair0) {
+    constexpr int NT = kPairThreads;
+    __shared__ double red[4][NT / 64];
+    const int64_t pair = pair0 + blockIdx.x;
+    int64_t at[3];
+    bool bad = false;
+    for (int i = 0; i < 3; ++i) {
+        const int64_t s = 2 * pair + i;
+        at[i] = q.first ? (int64_t)q.first[s] : s * (a.rows / (2 * q.pairs));
+        if (at[i] < 0 || at[i] > a.rows || (i && at[i] < at[i - 1])) bad = true;
+    }
+    if (bad)
+        for (int i = 0; i < 3; ++i) at[i] = min(max(at[i], (int64_t)0), a.rows);
+    const float2 c2 = a.log2_tau;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};   // sums of l - ref, rows, of the two sequences
+    for (int64_t r = at[0] + threadIdx.x; r < at[2] && !bad; r += NT) {
+        const int y = a.tokens[r];
+        if (y == -1) continue;
+        double l = (double)kNan;
+        RowSlope o{0.f, kNan, kNan, 1};
+        if (y >= 0 && y < a.V) {
+            const PartStats* stats = b.p.stats + r * b.p.parts;
+            const float zy = stats[y / b.p.len].zy;
+            o.m = zy;
+            for (int c = 0; c < b.p.parts; ++c) o.m = fmaxf(o.m, stats[c].m);
+            Sums sum;
+            for (int c = 0; c < b.p.parts; ++c) sum.s += part_sums<false>(stats[c], o.m, c2, 0.f).s;
+            const RowEnd e = row_end(o.m, zy, sum, a.inv_tau);
+            l = e.l;
+            const Slopes sl = slopes_of(e, Goal{0.0, 1.0, 0.0}, a.inv_tau);
+            o.a0 = sl.a0;
+            o.gy = sl.gy;
+        }
+        b.slope[r] = o;   // of l itself
+        if (q.ref_logprob) l -= (double)q.ref_logprob[r];
+        const int which = r >= at[1] ? 1 : 0;
+        s[0] += which ? 0.0 : l;
+        s[1] += which ? l : 0.0;
+        s[2 + which] += 1.0;
+    }
+    block_all<NT, 4>(s, red, AddOp());
+    double n[2] = {1.0, 1.0};
+    if (q.mean)
+        for (int i = 0; i < 2; ++i) n[i] = fmax(s[2 + i], 1.0);
+    const double chosen = bad ? (double)kNan : s[0] / n[0], rejected = bad ? (double)kNan : s[1] / n[1];
+    const double u = chosen - rejected - q.margin, h = q.beta * u;
+    double loss, slope;   // slope: by u
+    if (q.form == HBSJD_PREFERENCE_SIGMOID) {
+        loss = (1.0 - q.smoothing) * softplus(-h);
+        slope = -(1.0 - q.smoothing) * logistic(-h);
+        if (q.smoothing > 0.0) {
+            loss += q.smoothing * softplus(h);
+            slope += q.smoothing * logistic(h);
+        }
+        slope *= q.beta;
+    } else if (q.form == HBSJD_PREFERENCE_HINGE) {
+        loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+        slope = h < 1.0 ? -q.beta : 0.0;
+    } else {
+        const double d = u - 0.5 / q.beta;
+        loss = d * d;
+        slope = 2.0 * d;
+    }
+    const float w = q.weight ? q.weight[pair] : 1.f;
+    const float value = w == 0.f ? 0.f : (float)(w * loss);
+    if (threadIdx.x == 0) {
+        if (q.loss) q.loss[pair] = value;
+        if (q.log_ratio) {
+            q.log_ratio[2 * pair] = (float)chosen;
+            q.log_ratio[2 * pair + 1] = (float)rejected;
+        }
+    }
+    if (!a.grad) return;
+    const bool ok = value > -INFINITY && value < INFINITY;
+    const double by_l[2] = {w * slope / n[0], -w * slope / n[1]};
+    for (int64_t r = at[0] + threadIdx.x; r < (bad ? max(at[1], at[2]) : at[2]); r += NT) {
+        if (a.tokens[r] == -1) continue;
+        RowSlope o{0.f, kNan, kNan, 1};
+        if (ok && !bad) {
+            o = b.slope[r];
+            const double f = by_l[r >= at[1] ? 1 : 0];
+            o.a0 = w == 0.f || f == 0.0 ? 0.f : (float)(o.a0 * f);
+            o.gy = w == 0.f || f == 0.0 ? 0.f : (float)(o.gy * f);
+        }
+        b.slope[r] = o;
+    }
+}
+
+// The second reading: the gradient. The last rows come first: the first reading
+// has left them in the last-level cache.
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_pair_grad(TokenArgs a, PairArgs b, int chunks, int len, int64_t r1) {
+    const int row = blockIdx.x / chunks, c = blockIdx.x - row * chunks;
+    const int64_t r = r1 - 1 - row;
+    const int first = c * len, V = min(len, a.V - first);
+    const T* z = (const T*)a.logits + r * a.ld + first;
+    T* g = (T*)a.grad + r * a.ld_grad + first;
+    const RowSlope o = b.slope[r];
+    const float a0 = uniform(o.a0), gy = uniform(o.gy), m = uniform(o.m);
+    if (!uniform(o.used) || (a0 == 0.f && gy == 0.f)) return fill_row<NT>(g, V, 0.f);
+    if (a0 != a0 || gy != gy) return fill_row<NT>(g, V, kNan);
+    TokenRow<T, NT, NV> part;
+    part.load(z, V);
+    part.find(a.tokens[r] - first, V);
+    part.template store<false>(g, z, V, m, a.log2_tau, 0.f, a0, 0.f, gy);
+}
+
+// ---- how a call runs
+
+struct Plan {
+    int parts = 0, len = 0;
+    int64_t slab = 0;   // rows that the workspace holds at a time
+};
+constexpr int kPart = 16384;   // entries of a part at most
+
+// parts of up to kPart entries, more of them until there are 512 workgroups, of
+// 4096 entries at least and 64 at most (a lane each joins them)
+void cut(Plan& p, int64_t rows, int V) {
+    p.parts = (V + kPart - 1) / kPart;
+    while (rows * p.parts < 512 && V / (2 * p.parts) >= 4096 && p.parts <= 32) p.parts *= 2;
+    p.len = ((V + p.parts - 1) / p.parts + 7) / 8 * 8;
+    p.parts = (V + p.len - 1) / p.len;
+}
+
+Plan plan_of(int64_t rows, int V, int32_t elem) {
+    Plan p;
+    const int64_t size = elem_size(elem);
+    const int64_t held = 1024 * 16 * (16 / size);
+    if (V * size <= 128 << 10 || (V <= held && rows >= 112)) return p;
+    cut(p, rows, V);
+    p.slab = std::min<int64_t>(rows, (1 << 20) / p.parts);
+    return p;
+}
+
+// f(threads, vectors a thread) of the workgroups that hold rows of V entries
+template <typename T, typename F> void by_size(int V, F f) {
+    using std::integral_constant;
+    const int vecs = V / kVec<T>;
+#define HELD(nt, nv) f(integral_constant<int, nt>{}, integral_constant<int, nv>{})
+    if (vecs <= 64 * 2) HELD(64, 2);
+    else if (vecs <= 64 * 8) HELD(64, 8);
+    else if (vecs <= 256 * 4) HELD(256, 4);
+    else if (vecs <= 256 * 8) HELD(256, 8);
+    else if (vecs <= 512 * 8) HELD(512, 8);
+    else if (vecs <= 1024 * 8) HELD(1024, 8);
+    else HELD(1024, 16);
+#undef HELD
+}
+
+template <typename T, bool Ent> void go(const TokenArgs& a, void* ws, hipStream_t s) {
+    const Plan plan = plan_of(a.rows, a.V, a.elem);
+    if (plan.parts) {
+        constexpr int NT = 512, NV = kPart / kVec<T> / NT;
+        const PartsArgs p{plan.parts, plan.len, (PartStats*)ws};
+        for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
+            const dim3 grid((unsigned)(std::min(plan.slab, a.rows - r0) * p.parts));
+            hipLaunchKernelGGL((k_token_part<T, NT, NV, Ent>), grid, dim3(NT), 0, s, a, p, r0);
+            hipLaunchKernelGGL((k_token_rest<T, NT, NV, Ent>), grid, dim3(NT), 0, s, a, p, r0);
+        }
+        return;
+    }
+    const size_t lds = a.grad ? resident_lds(0, a.V * sizeof(T)) : 0;
+    by_size<T>(a.V, [&](auto nt, auto nv) {
+        by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+            hipLaunchKernelGGL((k_token<T, decltype(nt)::value, decltype(nv)::value, Ent>), grid,
+                               dim3(decltype(nt)::value), lds, s, a, r0);
+        });
+    });
+}
+
+template <typename T> void go_token(const TokenArgs& a, void* ws, hipStream_t s) {
+    const bool entropy = a.entropy || a.entropy_weight || (a.advantage && a.bonus > 0.f);
+    if (entropy) go<T, true>(a, ws, s);
+    else go<T, false>(a, ws, s);
+}
+
+Plan pair_plan(int64_t rows, int V) {
+    Plan p;
+    cut(p, rows, V);
+    return p;
+}
+
+// workgroups of the second reading take 256 KB / 16 = 16 KB of a row
+template <typename T> constexpr int kChunk2 = 256 * 4 * kVec<T>;
+
+template <typename T> void go_pairs(const TokenArgs& a, const PreferenceArgs& q, void* ws, hipStream_t s) {
+    const Plan plan = pair_plan(a.rows, a.V);
+    PairArgs b;
+    b.slope = (RowSlope*)ws;
+    b.p = PartsArgs{plan.parts, plan.len, (PartStats*)(b.slope + a.rows)};
+    by_size<T>(plan.len, [&](auto nt, auto nv) {
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        if constexpr (NT <= 512)   // a part's entries are no more
+            by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+                hipLaunchKernelGGL((k_pair_stats<T, NT, NV>), grid, dim3(NT), 0, s, a, q, b, r0);
+            }, plan.parts);
+    });
+    by_slabs(q.pairs, [&](int64_t p0, dim3 grid) {
+        hipLaunchKernelGGL(k_pair, grid, dim3(kPairThreads), 0, s, a, q, b, p0);
+    });
+    if (!a.grad) return;
+    const int chunks = (a.V + kChunk2<T> - 1) / kChunk2<T>;
+    const int len = ((a.V + chunks - 1) / chunks + 7) / 8 * 8;
+    by_size<T>(len, [&](auto nt, auto nv) {
+        constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+        if constexpr (NT * NV <= 1024) {   // up to kChunk2
+            const int64_t slab = (1 << 21) / chunks;
+            for (int64_t r1 = a.rows; r1 > 0; r1 -= slab) {
+                const dim3 grid((unsigned)(std::min(slab, r1) * chunks));
+                hipLaunchKernelGGL((k_pair_grad<T, NT, NV>), grid, dim3(NT), 0, s, a, b, chunks, len, r1);
+            }
+        }
+    });
+}
+
+}  // namespace
+
+size_t token_workspace(int64_t rows, int V, int32_t elem) {
+    const Plan p = plan_of(rows, V, elem);
+    return (size_t)p.slab * p.parts * sizeof(PartStats);
+}
+
+void token_rows(const TokenArgs& a, void* workspace, hipStream_t s) {
+    if (a.elem == HBSJD_ELEM_F32) go_token<float>(a, workspace, s);
+    else if (a.elem == HBSJD_ELEM_BF16) go_token<Bf16>(a, workspace, s);
+    else go_token<F16>(a, workspace, s);
+}
+
+size_t preference_workspace(int64_t rows, int V, int32_t) {
+    const Plan p = pair_plan(rows, V);
+    return (size_t)rows * (sizeof(RowSlope) + p.parts * sizeof(PartStats));
+}
+
+void preference_rows(const TokenArgs& a, const PreferenceArgs& p, void* workspace, hipStream_t s) {
+    if (a.elem == HBSJD_ELEM_F32) go_pairs<float>(a, p, workspace, s);
+    else if (a.elem == HBSJD_ELEM_BF16) go_pairs<Bf16>(a, p, workspace, s);
+    else go_pairs<F16>(a, p, workspace, s);
+}
+
+}  // namespace hbsjd

@@ -1,0 +1,230 @@
+"""The norm of lists of tensors and their clipping, against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+from tests.row_operators_ref import ROUND, U
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+NAMES = {v: k for k, v in TYPES.items()}
+
+
+def P():
+    import paper_2608_18183_amd
+    return paper_2608_18183_amd
+
+
+def tensors(rng, sizes, types, offset=0):
+    """Tensors that start `offset` entries behind an aligned address, each in a buffer
+    with room around it."""
+    out = []
+    for j, n in enumerate(sizes):
+        t = TYPES[types[j % len(types)]]
+        buf = torch.full((n + offset + 40,), 7.0, dtype=t, device="cuda")
+        g = buf[offset:offset + n]
+        g.copy_(torch.from_numpy(rng.normal(0, 0.1, n).astype(np.float32)))
+        out.append((g, buf))
+    return [g for g, _ in out], [b for _, b in out]
+
+
+def around(buf, g):
+    """What lies around a tensor is as it was."""
+    a = g.storage_offset()
+    return bool((buf[:a] == 7).all()) and bool((buf[a + g.numel():] == 7).all())
+
+
+def norm64(grads, order):
+    x = np.concatenate([g.detach().double().cpu().numpy().ravel() for g in grads] + [np.zeros(1)])
+    return math.sqrt(float((x * x).sum())) if order == 2 else float(np.abs(x).max())
+
+
+def check_norm(norm, want):
+    # the sum's own error in 64 bits is nothing next to the one rounding to fp32
+    assert abs(float(norm) - want) <= 1.001 * U * want
+
+
+def check_scaled(got, g, scale):
+    """Two roundings in fp32 (the factor, the product), one to the type."""
+    step, least = ROUND[NAMES[g.dtype]]
+    w = g.double() * scale
+    bound = w.abs() * (2 * U + step) * 1.001 + least
+    assert bool(((got.double() - w).abs() <= bound).all())
+
+
+LISTS = [[1], [5], [16384], [0], [0, 3, 0, 0, 7, 0], [2047, 2048, 2049], [32767, 32768, 32769, 1, 2],
+         [1 << 20, 3, 1 << 20], list(range(130)), [64] * 400, [5_000_001, 11]]
+
+
+@pytest.mark.parametrize("offset", [0, 1, 3])
+@pytest.mark.parametrize("types", [("f32",), ("bf16",), ("f16",), ("f32", "bf16", "f16")])
+@pytest.mark.parametrize("sizes", range(len(LISTS)))
+def test_norm_and_clip(sizes, types, offset):
+    rng = np.random.default_rng(sizes)
+    grads, bufs = tensors(rng, LISTS[sizes], types, offset)
+    before = [g.clone() for g in grads]
+    for order in (2, math.inf):
+        want = norm64(grads, order)
+        check_norm(P().hbsjd_grad_norm(grads, order=order), want)
+        # above the norm: nothing happens
+        check_norm(P().hbsjd_clip_grads(grads, 2 * want + 1, order=order), want)
+        assert all(torch.equal(a, b) for a, b in zip(grads, before))
+        # into other tensors, laid out otherwise: copies, then scaled
+        out, obufs = tensors(rng, LISTS[sizes], types, 2)
+        P().hbsjd_clip_grads(grads, 2 * want + 1, order=order, out=out)
+        assert all(torch.equal(a, b) for a, b in zip(out, before))
+        check_norm(P().hbsjd_clip_grads(grads, 0.3 * want, order=order, out=out), want)
+        scale = float(np.float32(0.3 * want)) / want if want else 1.0
+        for o, g, buf in zip(out, before, obufs):
+            check_scaled(o, g, scale)
+            assert around(buf, o)
+        assert all(torch.equal(a, b) for a, b in zip(grads, before))
+    check_norm(P().hbsjd_clip_grads(grads, 0.3 * want, order=math.inf), want)
+    for g, b, buf in zip(grads, before, bufs):
+        check_scaled(g, b, scale)
+        assert around(buf, g)
+
+
+def test_nothing():
+    assert float(P().hbsjd_grad_norm([])) == 0
+    assert float(P().hbsjd_clip_grads([], 1.0)) == 0
+    assert float(P().hbsjd_clip_grads([torch.zeros(0, device="cuda")], 0.0)) == 0
+
+
+def test_shapes_and_orders_of_entries():
+    """Matrices, transposed ones, single numbers; views with gaps are refused."""
+    g = torch.Generator("cuda").manual_seed(1)
+    a = torch.randn((30, 50), generator=g, device="cuda")
+    b = torch.randn((4, 6, 5), generator=g, device="cuda").permute(2, 0, 1)
+    c = torch.randn((), generator=g, device="cuda")
+    grads = [a.t(), b, c, a.new_empty(1, 3, 1).fill_(2.0)]
+    before = [t.clone() for t in grads]
+    want = norm64(grads, 2)
+    check_norm(P().hbsjd_clip_grads(grads, want / 2), want)
+    for t, s in zip(grads, before):
+        check_scaled(t, s, float(np.float32(want / 2)) / want)
+    for bad in (a[:, :20], a[::2], torch.zeros(1, device="cuda").expand(5), a.double(), a.int(), a.cpu(), 3.0, None,
+                torch.sparse_coo_tensor([[0]], [1.0], (4,), device="cuda")):
+        with pytest.raises(ValueError):
+            P().hbsjd_grad_norm([a, bad])
+        with pytest.raises(ValueError):
+            P().hbsjd_clip_grads([bad], 1.0)
+    for out in ([], [a], [a.t(), a], [a.clone(), b.contiguous()], [a.clone(), b.half()], [a.clone(), None]):
+        with pytest.raises(ValueError):
+            P().hbsjd_clip_grads([a, b], 1.0, out=out)
+    for order in (0, 1, 3, -2, float("nan")):
+        with pytest.raises(ValueError):
+            P().hbsjd_grad_norm([a], order=order)
+
+
+def test_overlapping_tensors_are_not_written():
+    x = torch.randn(1000, device="cuda")
+    keep = x.clone()
+    out = torch.empty_like(x)
+    for grads, to in (([x, x], None), ([x[:600], x[500:]], None), ([x[500:], x[:501]], None),
+                      ([x[:10], x[20:30]], [out[:10], out[5:15]]), ([x[:100], x[200:300]], [x[200:300], x[:100]]),
+                      ([x[:100]], [x[50:150]])):
+        with pytest.raises(P().HbsjdError) as e:
+            P().hbsjd_clip_grads(grads, 0.0, out=to)
+        assert e.value.code == "EINVAL"
+    assert torch.equal(x, keep)
+    # read alone they may, and a tensor may be its own output beside others
+    check_norm(P().hbsjd_grad_norm([x, x]), norm64([x, x], 2))
+    P().hbsjd_clip_grads([x[:600], x[500:700]], 0.5, out=[out[:600], out[700:900]])
+    P().hbsjd_clip_grads([x[:600], x[600:700]], 0.5, out=[x[:600], out[600:700]])
+    assert not torch.equal(x[:600], keep[:600]) and torch.equal(x[600:], keep[600:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_numbers_that_are_none(dtype):
+    """NaN and infinities show in the norm, and nothing is scaled."""
+    for value in (math.nan, math.inf, -math.inf):
+        for at in (0, 77, 70000):
+            g = [torch.full((70001,), 0.5, dtype=TYPES[dtype], device="cuda") for _ in range(3)]
+            g[1][at] = value
+            keep = [t.clone() for t in g]
+            for order in (2, math.inf):
+                norm = float(P().hbsjd_clip_grads(g, 0.1, order=order))
+                assert math.isnan(norm) if math.isnan(value) else norm == math.inf
+                assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(g, keep))
+                out = [torch.empty_like(t) for t in g]
+                P().hbsjd_clip_grads(g, 0.1, order=order, out=out)
+                assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(out, keep))
+
+
+def test_squares_past_fp32():
+    """Squares that fp32 has no numbers for, and a norm that it has none for."""
+    g = [torch.full((1000,), 1e30, device="cuda"), torch.full((10,), 1e-30, device="cuda")]
+    check_norm(P().hbsjd_grad_norm(g), norm64(g, 2))
+    check_norm(P().hbsjd_grad_norm(g[1:]), norm64(g[1:], 2))
+    P().hbsjd_clip_grads(g, 1.0)
+    check_norm(P().hbsjd_grad_norm(g), 1.0)
+    big = torch.full((100,), 3e38, device="cuda")
+    assert float(P().hbsjd_clip_grads([big], 1e38)) == math.inf
+    check_scaled(big, torch.full_like(big, 3e38), float(np.float32(1e38)) / (10 * float(np.float32(3e38))))
+    zero = torch.zeros(100, device="cuda")
+    assert float(P().hbsjd_clip_grads([zero], 0.0)) == 0 and bool((zero == 0).all())
+    x = torch.randn(100, device="cuda")
+    P().hbsjd_clip_grads([x], 0.0)
+    assert bool((x == 0).all())
+    for limit in (-1.0, math.nan):
+        with pytest.raises(P().HbsjdError) as e:
+            P().hbsjd_clip_grads([x], limit)
+        assert e.value.code == "EINVAL"
+    keep = x.copy_(torch.ones(100)).clone()
+    P().hbsjd_clip_grads([x], math.inf)
+    assert torch.equal(x, keep)
+
+
+def test_more_entries_than_32_bits_count():
+    """One bf16 tensor of 2^32 + 77 entries: its last ones count and are scaled."""
+    n = 2 ** 32 + 77
+    x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    x[-1], x[-70], x[0], x[2 ** 31 + 5] = 3.0, 4.0, 12.0, 84.0
+    check_norm(P().hbsjd_clip_grads([x], 42.5), 85.0)
+    assert [float(x[i]) for i in (-1, -70, 0, 2 ** 31 + 5)] == [1.5, 2.0, 6.0, 42.0]
+    assert int((x != 0).sum()) == 4
+
+
+def test_captured_streams_and_the_same_bits():
+    gen = torch.Generator("cuda").manual_seed(3)
+    grads = [torch.randn(n, generator=gen, device="cuda").to(t)
+             for n, t in ((100_003, torch.float32), (7, torch.bfloat16), (1 << 21, torch.float16)) for _ in range(60)]
+    outs = [[torch.empty_like(g) for g in grads] for _ in range(2)]
+    P().hbsjd_clip_grads(grads, 1.0, out=outs[0])
+    torch.cuda.synchronize()
+    graphs = []
+    for j in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            norm = P().hbsjd_clip_grads(grads, 1.0 + j, out=outs[j])
+        graphs.append((g, norm))
+    other = [torch.empty_like(g) for g in grads]
+    s = torch.cuda.Stream()
+    for rep in range(3):
+        for g in grads:
+            g.mul_(1.5)
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for j in range(2):
+            norm = P().hbsjd_clip_grads(grads, 1.0 + j, out=other, stream=s)
+            s.synchronize()
+            assert torch.equal(norm, graphs[j][1])
+            assert all(torch.equal(a, b) for a, b in zip(other, outs[j])), (rep, j)
+        assert torch.equal(P().hbsjd_grad_norm(grads), graphs[0][1])
+
+
+def test_autograd_sees_what_is_written():
+    x = torch.randn(50, device="cuda", requires_grad=True)
+    y = x.exp()
+    P().hbsjd_clip_grads([y.detach()], 1e9)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    y, out = x.exp(), torch.empty(50, device="cuda")
+    P().hbsjd_clip_grads([y.detach()], 0.1, out=[out])
+    y.sum().backward()
+    assert out._version > 0 and not P().hbsjd_grad_norm([x]).requires_grad
