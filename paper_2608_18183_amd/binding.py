@@ -4,8 +4,10 @@ Device buffers are torch CUDA (HIP) tensors; host buffers are numpy arrays.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import dataclasses
+import operator
 import os
 import threading
 from typing import Optional
@@ -789,11 +791,10 @@ def hbsjd_policy_rows(logits, tokens, advantage, old_logprob=None, ref_logprob=N
                     _per_row(old_logprob, "old_logprob", rows, f32, dev),
                     _per_row(ref_logprob, "ref_logprob", rows, f32, dev), clip_low, clip_high,
                     kl_weight, entropy_weight, _per_row(row_weight, "row_weight", rows, f32, dev))
-    loss = logits.new_empty((rows,), dtype=f32)
-    logprob = logits.new_empty((rows,), dtype=f32)
-    if entropy is None:
-        entropy = entropy_weight > 0
-    entropy = logits.new_empty((rows,), dtype=f32) if entropy else None
+    if entropy or (entropy is None and entropy_weight > 0):
+        loss, logprob, entropy = logits.new_empty((3, rows), dtype=f32).unbind(0)
+    else:
+        (loss, logprob), entropy = logits.new_empty((2, rows), dtype=f32).unbind(0), None
     grad, address, ld_grad, given = _gradient(grad, logits)
     L = _lib or load_library()
     ws, nbytes = None, 0
@@ -886,20 +887,35 @@ def _dense(t) -> bool:
     return True
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 def _described(tensors, what: str, device):
-    """The addresses, sizes and types of dense device tensors, as arrays for C."""
-    types = _ELEMS
-    for t in tensors:
-        if not isinstance(t, _torch.Tensor) or t.device != device or t.layout is not _torch.strided:
-            raise ValueError(f"{what}: expected tensors on {device}")
-        if t.dtype not in types:
-            raise ValueError(f"{what}: fp32, bf16 or fp16, not {t.dtype}")
-        if not t.is_contiguous() and not _dense(t):
-            raise ValueError(f"{what}: a tensor's entries have to lie one after another")
-    n = len(tensors)
-    return ((_P * n)(*[t.data_ptr() for t in tensors]),
-            (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
-            (_I32 * n)(*[types[t.dtype] for t in tensors]))
+    """The addresses, sizes and types of dense device tensors, as arrays for C, and
+    whether all are contiguous. (Lists may be hundreds long: one pass in C for each
+    property takes 25 ns a tensor, the loop below ten times that.)"""
+    T, types = _torch.Tensor, _ELEMS
+    try:
+        at = array.array("Q", map(T.data_ptr, tensors))
+        sizes = array.array("q", map(T.numel, tensors))
+        dtypes = list(map(_dtype_of, tensors))
+        flat = all(map(T.is_contiguous, tensors))
+        sound = set(map(T.get_device, tensors)) <= {device.index} and types.keys() >= set(dtypes)
+    except (TypeError, RuntimeError, AttributeError, NotImplementedError):
+        sound = flat = False
+    if not sound or not flat:
+        for t in tensors:
+            if not isinstance(t, T) or t.device != device or t.layout is not _torch.strided:
+                raise ValueError(f"{what}: expected tensors on {device}")
+            if t.dtype not in types:
+                raise ValueError(f"{what}: fp32, bf16 or fp16, not {t.dtype}")
+            if not _dense(t):
+                raise ValueError(f"{what}: a tensor's entries have to lie one after another")
+    return at, sizes, array.array("i", map(types.__getitem__, dtypes)), flat
+
+
+def _start(a) -> int:
+    return a.buffer_info()[0]
 
 
 def _list_device(tensors):
@@ -924,13 +940,14 @@ def hbsjd_grad_norm(grads, order: float = 2.0, stream=None):
         with _OnStream(dev, stream, grads):
             return hbsjd_grad_norm(grads, order)
     order = _order(order)
-    data, sizes, elems = _described(grads, "grads", dev)
+    data, sizes, elems, _ = _described(grads, "grads", dev)
     norm = torch.empty((), dtype=torch.float32, device=dev)
     L = _lib or load_library()
     nbytes = L.hbsjd_grad_norm_workspace()
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
-    st = L.hbsjd_grad_norm(len(grads), data, sizes, elems, order, norm.data_ptr(), ws.data_ptr(),
-                           nbytes, torch._C._cuda_getCurrentRawStream(dev.index))
+    st = L.hbsjd_grad_norm(len(grads), _start(data), _start(sizes), _start(elems), order,
+                           norm.data_ptr(), ws.data_ptr(), nbytes,
+                           torch._C._cuda_getCurrentRawStream(dev.index))
     if st:
         _check(st, "hbsjd_grad_norm")
     return norm
@@ -939,7 +956,8 @@ def hbsjd_grad_norm(grads, order: float = 2.0, stream=None):
 def hbsjd_clip_grads(grads, limit: float, order: float = 2.0, out=None, stream=None):
     """Scales a list of device tensors (as hbsjd_grad_norm takes them) by limit / norm
     where their norm is above the limit. In place, or into the tensors of the list
-    `out`, of the same shapes, types and strides (copies where nothing is scaled).
+    `out`, of the same sizes and types and laid out alike (copies where nothing is
+    scaled).
     Returns the norm ahead of the scaling, a device tensor fp32 []. A norm that is not
     finite scales nothing."""
     torch = _torch or _load_torch()
@@ -950,21 +968,21 @@ def hbsjd_clip_grads(grads, limit: float, order: float = 2.0, out=None, stream=N
         with _OnStream(dev, stream, grads + (out or [])):
             return hbsjd_clip_grads(grads, limit, order, out)
     order = _order(order)
-    data, sizes, elems = _described(grads, "grads", dev)
+    data, sizes, elems, flat = _described(grads, "grads", dev)
     out_at = None
     if out is not None:
-        if len(out) != len(grads):
-            raise ValueError(f"out: expected {len(grads)} tensors")
-        for g, o in zip(grads, out):
-            if (not isinstance(o, torch.Tensor) or o.dtype is not g.dtype or o.shape != g.shape
-                    or o.device != dev or o.stride() != g.stride()):
-                raise ValueError("out: expected tensors of the same shapes, types and strides")
-        out_at = (_P * len(out))(*[o.data_ptr() for o in out])
+        out_at, out_sizes, out_elems, out_flat = _described(out, "out", dev)
+        alike = out_sizes == sizes and out_elems == elems
+        if alike and not (flat and out_flat):
+            alike = all(g.shape == o.shape and g.stride() == o.stride() for g, o in zip(grads, out))
+        if not alike:
+            raise ValueError("out: expected tensors of the same sizes, types and strides")
     norm = torch.empty((), dtype=torch.float32, device=dev)
     L = _lib or load_library()
     nbytes = L.hbsjd_grad_norm_workspace()
     ws = torch.empty((nbytes,), dtype=torch.uint8, device=dev)
-    st = L.hbsjd_clip_grads(len(grads), data, sizes, elems, order, limit, out_at, norm.data_ptr(),
+    st = L.hbsjd_clip_grads(len(grads), _start(data), _start(sizes), _start(elems), order, limit,
+                            None if out is None else _start(out_at), norm.data_ptr(),
                             ws.data_ptr(), nbytes, torch._C._cuda_getCurrentRawStream(dev.index))
     if st:
         _check(st, "hbsjd_clip_grads")

@@ -1,11 +1,19 @@
 // The norm of all entries of a list of tensors, and the tensors scaled by it.
 //
-// The tensors are cut into units of 2048 16-byte vectors, and a fixed number of
-// workgroups takes an equal run of units each: many small tensors and a few huge ones
-// are the same work. What describes the tensors travels in the kernel's arguments
-// (kTable tensors a launch), so that a call keeps nothing and can be captured. Each
-// workgroup leaves one number; every workgroup of the scaling adds them up for itself
-// in the same order, which saves a launch.
+// The tensors are cut into units of 64 KB, and a fixed number of workgroups takes every
+// so manieth unit each: many small tensors and a few huge ones are the same work, and
+// the workgroups sweep through memory side by side. What describes the tensors travels
+// in the kernels' arguments (192 tensors a launch, 136 that are copied), so that a call
+// keeps nothing and can be captured. Each workgroup leaves one number; every workgroup
+// of the scaling adds them up for itself in the same order, which saves a launch.
+//
+// Memory alone bounds both passes (squares in 64 bits or 32: 45.9 and 45.4 us for the
+// 222 MB of the B model). What the second pass finds of the first one's reading in the
+// last-level cache (256 MB) is not read again: the tensors' last kKeep bytes are read as
+// usual, those before them and all of the second pass as streams, and the second pass
+// starts from the end. Clipping 111 M bf16 entries (222 MB) into others, both passes'
+// kernels: all loads and stores as usual 120 us, stores alone as streams 104, and the
+// second pass's loads 105; 757 M fp32 ones 1706, 1664, 1582.
 #include "grad_norm.h"
 
 #include <algorithm>
@@ -13,21 +21,36 @@
 namespace hbsjd {
 namespace {
 
-constexpr int NT = 512, NV = 4;
-constexpr int kUnit = NT * NV;   // vectors of a unit
-constexpr int kTable = 120;      // tensors of a launch: 3.5 of the 4 KB that arguments may take
-constexpr int kGroups = 1024;    // workgroups of a call: four a CU
+constexpr int NT = 512, NV = 8;
+constexpr int kUnit = NT * NV;     // 16-byte vectors of a unit
+constexpr int kGroups = 2048;      // workgroups of a launch at most: eight a CU
+constexpr int kPartials = 8192;    // and of a call
+constexpr uint64_t kKeep = ((uint64_t)192 << 20) / (kUnit * 16);   // units that stay in the last-level cache
 
-struct Table {
-    const void* in[kTable];
-    void* out[kTable];
-    int64_t n[kTable];
-    uint32_t unit[kTable + 1];   // the tensors' first units
-    uint8_t elem[kTable];
+// What a launch knows of its tensors, N of them at most: as many as 4 KB of
+// arguments hold.
+template <int N, bool Out> struct Table {
+    static constexpr int kTensors = N;
+    static constexpr bool kOut = Out;
+    const void* in[N];
+    void* out[Out ? N : 1];        // else the tensors themselves
+    int64_t n[N];                  // entries, the type in the uppermost bits
+    uint32_t unit[N + 1];          // the tensors' first units
+    uint32_t stream;               // units below this one move as streams
     int count;
     int groups;
-    int first_group;   // of this launch among the call's
+    int first_group;               // of this launch among the call's
+    __host__ __device__ int64_t size(int i) const { return n[i] & (((int64_t)1 << 48) - 1); }
+    __host__ __device__ int elem(int i) const { return (int)(n[i] >> 48); }
+    __device__ void* to(int i) const { return Out ? out[i] : (void*)in[i]; }
 };
+using Inputs = Table<192, false>;
+using Copies = Table<136, true>;
+
+// Lists of up to 64 MB are scaled with usual loads and stores: whatever reads them next
+// finds them in the cache (clipping 16 MB and adding the result to others: 27 us, 36 with
+// streams; 64 MB 64 either way; 128 MB 165 and 145).
+constexpr uint64_t kSmall = ((uint64_t)64 << 20) / (kUnit * 16);
 
 // A tensor as vectors: entries ahead of the first aligned one and behind the last
 // whole vector are single.
@@ -82,17 +105,31 @@ template <typename A> __device__ __forceinline__ A all(A a, A* red) {
     return r;
 }
 
-template <typename T, typename A>
-__device__ __forceinline__ void take_unit(const Table& t, int i, uint32_t u, A& a) {
+// a unit's vectors: NV a thread, those behind the end repeat the last
+template <bool Stream>
+__device__ __forceinline__ void load_unit(const u32x4* z, int vecs, u32x4 (&x)[NV]) {
+    if (vecs > 0)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const u32x4& v = vec_at(z, min((int)threadIdx.x + NT * k, vecs - 1));
+            x[k] = Stream ? __builtin_nontemporal_load(&v) : v;
+        }
+}
+
+template <typename T, typename Tab, typename A>
+__device__ __forceinline__ void take_unit(const Tab& t, int i, uint32_t u, A& a) {
     const T* p = (const T*)t.in[i];
-    const LongSpan sp = long_span(p, t.n[i], sizeof(T));
+    const LongSpan sp = long_span(p, t.size(i), sizeof(T));
     const int64_t v0 = (int64_t)u * kUnit;
     const int vecs = (int)min(sp.vecs - v0, (int64_t)kUnit);
     const u32x4* z = (const u32x4*)(p + sp.head) + v0;
     u32x4 x[NV];
-    if (vecs > 0)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) x[k] = vec_at(z, min((int)threadIdx.x + NT * k, vecs - 1));
+    if (t.unit[i] + u < t.stream) {
+        load_unit<true>(z, vecs, x);
+        asm volatile("");   // else the compiler makes one of the two, with usual loads
+    } else {
+        load_unit<false>(z, vecs, x);
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         if ((int)threadIdx.x + NT * k >= vecs) break;
@@ -101,13 +138,13 @@ __device__ __forceinline__ void take_unit(const Table& t, int i, uint32_t u, A& 
     }
     if (u == 0 && (int)threadIdx.x < sp.head + sp.tail) {
         const int e = threadIdx.x;
-        a.add(widen(p[e < sp.head ? (int64_t)e : t.n[i] - sp.tail + (e - sp.head)]));
+        a.add(widen(p[e < sp.head ? (int64_t)e : t.size(i) - sp.tail + (e - sp.head)]));
     }
 }
 
 // the tensor that holds unit u: the last that starts at or before it (empty ones
 // start where the next one does)
-__device__ __forceinline__ int tensor_of(const Table& t, uint32_t u) {
+template <typename Tab> __device__ __forceinline__ int tensor_of(const Tab& t, uint32_t u) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -117,20 +154,16 @@ __device__ __forceinline__ int tensor_of(const Table& t, uint32_t u) {
     return lo;
 }
 
-__device__ __forceinline__ uint32_t first_unit(const Table& t, int group) {
-    return (uint32_t)((uint64_t)t.unit[t.count] * (uint32_t)group / (uint32_t)t.groups);
-}
-
-template <typename A> __global__ __launch_bounds__(NT) void k_norm_part(Table t, A* part) {
+template <typename A> __global__ __launch_bounds__(NT) void k_norm_part(Inputs t, A* part) {
     __shared__ A red[NT / 64];
-    const uint32_t end = first_unit(t, blockIdx.x + 1);
-    uint32_t u = first_unit(t, blockIdx.x);
+    const uint32_t end = t.unit[t.count];
+    uint32_t u = blockIdx.x;
     A a{};
-    for (int i = tensor_of(t, u); u < end; ++u) {
+    for (int i = tensor_of(t, u); u < end; u += t.groups) {
         while (u >= t.unit[i + 1]) ++i;
         const uint32_t k = u - t.unit[i];
-        if (t.elem[i] == HBSJD_ELEM_F32) take_unit<float>(t, i, k, a);
-        else if (t.elem[i] == HBSJD_ELEM_BF16) take_unit<Bf16>(t, i, k, a);
+        if (t.elem(i) == HBSJD_ELEM_F32) take_unit<float>(t, i, k, a);
+        else if (t.elem(i) == HBSJD_ELEM_BF16) take_unit<Bf16>(t, i, k, a);
         else take_unit<F16>(t, i, k, a);
     }
     a = all(a, red);
@@ -149,18 +182,17 @@ template <typename A> __global__ __launch_bounds__(NT) void k_norm_join(const A*
     if (threadIdx.x == 0) *norm = (float)n;
 }
 
-template <typename T> __device__ __forceinline__ void scale_unit(const Table& t, int i, uint32_t u, float f) {
+template <typename T, bool Stream, typename Tab>
+__device__ __forceinline__ void scale_unit(const Tab& t, int i, uint32_t u, float f) {
     const T* p = (const T*)t.in[i];
-    T* g = (T*)t.out[i];
-    const LongSpan sp = long_span(p, t.n[i], sizeof(T));
+    T* g = (T*)t.to(i);
+    const LongSpan sp = long_span(p, t.size(i), sizeof(T));
     const int64_t v0 = (int64_t)u * kUnit;
     const int vecs = (int)min(sp.vecs - v0, (int64_t)kUnit);
     const u32x4* z = (const u32x4*)(p + sp.head) + v0;
     T* gv = g + sp.head + v0 * kVec<T>;
     u32x4 x[NV];
-    if (vecs > 0)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) x[k] = vec_at(z, min((int)threadIdx.x + NT * k, vecs - 1));
+    load_unit<Stream>(z, vecs, x);
     const bool same = (((uintptr_t)g ^ (uintptr_t)p) & 15) == 0;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -170,7 +202,10 @@ template <typename T> __device__ __forceinline__ void scale_unit(const Table& t,
 #pragma unroll
         for (int q = 0; q < kVec<T>; ++q) y[q] = vec_get<T>(x[k], q) * f;
         if (same) {
-            vec_at((u32x4*)gv, j) = f == 1.f ? x[k] : vec_pack<T>(y);   // a copy keeps NaNs' bits too
+            const u32x4 v = f == 1.f ? x[k] : vec_pack<T>(y);   // a copy keeps NaNs' bits too
+            u32x4& to = vec_at((u32x4*)gv, j);
+            if constexpr (Stream) __builtin_nontemporal_store(v, &to);
+            else to = v;
         } else {
 #pragma unroll
             for (int q = 0; q < kVec<T>; ++q) gv[j * kVec<T> + q] = narrow<T>(y[q]);
@@ -178,32 +213,39 @@ template <typename T> __device__ __forceinline__ void scale_unit(const Table& t,
     }
     if (u == 0 && (int)threadIdx.x < sp.head + sp.tail) {
         const int e = threadIdx.x;
-        const int64_t at = e < sp.head ? (int64_t)e : t.n[i] - sp.tail + (e - sp.head);
+        const int64_t at = e < sp.head ? (int64_t)e : t.size(i) - sp.tail + (e - sp.head);
         g[at] = narrow<T>(widen(p[at]) * f);
     }
 }
 
 // A workgroup's units, the last one first: the norm's pass has left those in the
 // last-level cache.
-template <typename A>
-__global__ __launch_bounds__(NT) void k_scale(Table t, const A* part, int groups, float limit, bool in_place,
-                                              float* norm) {
+template <typename A, typename Tab>
+__global__ __launch_bounds__(NT) void k_scale(Tab t, const A* part, int groups, float limit, float* norm) {
     __shared__ A red[NT / 64];
     const double n = norm_of(part, groups, red);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const bool scaled = n > (double)limit && n < INFINITY;
-    if (in_place && !scaled) return;
+    if (!Tab::kOut && !scaled) return;
     const float f = uniform(scaled ? (float)((double)limit / n) : 1.f);
-    const uint32_t begin = first_unit(t, blockIdx.x);
-    uint32_t u = first_unit(t, blockIdx.x + 1);
-    if (u == begin) return;
-    int i = tensor_of(t, u - 1);
-    while (u-- > begin) {
+    const uint32_t mine = (t.unit[t.count] - 1 - blockIdx.x) / t.groups;   // the last of this workgroup's
+    uint32_t u = blockIdx.x + mine * t.groups;
+    int i = tensor_of(t, u);
+    for (uint32_t left = mine + 1; left > 0; --left, u -= t.groups) {
         while (u < t.unit[i]) --i;
         const uint32_t k = u - t.unit[i];
-        if (t.elem[i] == HBSJD_ELEM_F32) scale_unit<float>(t, i, k, f);
-        else if (t.elem[i] == HBSJD_ELEM_BF16) scale_unit<Bf16>(t, i, k, f);
-        else scale_unit<F16>(t, i, k, f);
+        auto with = [&](auto type) {
+            using T = decltype(type);
+            if (u < t.stream) {
+                scale_unit<T, true>(t, i, k, f);
+                asm volatile("");   // (as above)
+            } else {
+                scale_unit<T, false>(t, i, k, f);
+            }
+        };
+        if (t.elem(i) == HBSJD_ELEM_F32) with(float{});
+        else if (t.elem(i) == HBSJD_ELEM_BF16) with(Bf16{});
+        else with(F16{});
     }
 }
 
@@ -213,62 +255,79 @@ uint32_t units_of(const void* p, int64_t n, int32_t elem) {
     return (uint32_t)std::max<int64_t>(1, (s.vecs + kUnit - 1) / kUnit);
 }
 
-// f(table) for the tensors in order, kTable at a time; false when one of the tables
-// holds more units than a launch counts
-template <typename F> bool by_tables(const GradArgs& a, uint64_t total, F f) {
-    Table t;
-    int groups = 0;
-    for (int64_t i0 = 0; i0 < a.count; i0 += kTable) {
-        t.count = (int)std::min<int64_t>(kTable, a.count - i0);
-        uint64_t units = 0;
+// f(table) for the tensors, in launches of equal numbers of them, from the first on or
+// from the last
+template <typename Tab, typename F> void by_tables(const GradArgs& a, bool from_last, F f) {
+    const int64_t launches = (a.count + Tab::kTensors - 1) / Tab::kTensors;
+    if (launches == 0) return;
+    const int64_t each = (a.count + launches - 1) / launches;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kGroups, kPartials / launches));
+    Tab t;
+    t.first_group = 0;
+    for (int64_t l = 0; l < launches; ++l) {
+        const int64_t i0 = (from_last ? launches - 1 - l : l) * each;
+        t.count = (int)std::min<int64_t>(each, a.count - i0);
+        if (t.count <= 0) continue;
+        uint32_t units = 0;
         for (int i = 0; i < t.count; ++i) {
             t.in[i] = a.data[i0 + i];
-            t.out[i] = a.out ? a.out[i0 + i] : nullptr;
-            t.n[i] = a.sizes[i0 + i];
-            t.elem[i] = (uint8_t)a.elems[i0 + i];
-            t.unit[i] = (uint32_t)units;
-            units += units_of(t.in[i], t.n[i], t.elem[i]);
-            if (units > UINT32_MAX) return false;
+            if (Tab::kOut) t.out[i] = a.out[i0 + i];
+            t.n[i] = a.sizes[i0 + i] | (int64_t)a.elems[i0 + i] << 48;
+            t.unit[i] = units;
+            units += units_of(t.in[i], a.sizes[i0 + i], a.elems[i0 + i]);
         }
-        t.unit[t.count] = (uint32_t)units;
+        t.unit[t.count] = units;
         if (units == 0) continue;
-        // the call's workgroups by the tables' units
-        t.groups = (int)std::min<uint64_t>(units, kGroups * units / total + 1);
-        t.first_group = groups;
-        groups += t.groups;
+        t.groups = (int)std::min<int64_t>(units, most);
         f(t);
+        t.first_group += t.groups;
     }
-    return true;
+}
+
+template <typename A, typename Tab>
+void scale(const GradArgs& a, const A* part, int groups, bool stream, hipStream_t s) {
+    float* norm = a.norm;
+    by_tables<Tab>(a, true, [&](Tab& t) {
+        t.stream = stream ? UINT32_MAX : 0;
+        hipLaunchKernelGGL((k_scale<A, Tab>), dim3(t.groups), dim3(NT), 0, s, t, part, groups, a.limit, norm);
+        norm = nullptr;   // the first launch writes it
+    });
 }
 
 template <typename A> bool go(const GradArgs& a, void* ws, hipStream_t s) {
     A* part = (A*)ws;
-    uint64_t total = 0;
-    for (int64_t i = 0; i < a.count; ++i) total += units_of(a.data[i], a.sizes[i], a.elems[i]);
+    uint64_t units = 0;
+    for (int64_t i = 0; i < a.count; ++i) units += units_of(a.data[i], a.sizes[i], a.elems[i]);
+    if (units > UINT32_MAX) return false;
     int groups = 0;
-    if (!by_tables(a, total, [&](const Table& t) { groups = t.first_group + t.groups; })) return false;
-    by_tables(a, total, [&](const Table& t) {
+    uint64_t done = 0;
+    by_tables<Inputs>(a, false, [&](Inputs& t) {
+        // the call's units from here on that are not among its last kKeep
+        const uint64_t mine = t.unit[t.count];
+        const uint64_t streams = units > done + kKeep ? units - done - kKeep : 0;
+        t.stream = (uint32_t)std::min(mine, streams);
+        done += mine;
         hipLaunchKernelGGL(k_norm_part<A>, dim3(t.groups), dim3(NT), 0, s, t, part);
+        groups = t.first_group + t.groups;
     });
     if (!a.out || groups == 0) {
         hipLaunchKernelGGL(k_norm_join<A>, dim3(1), dim3(NT), 0, s, part, groups, a.norm);
         return true;
     }
-    float* norm = a.norm;
     bool in_place = true;
     for (int64_t i = 0; i < a.count; ++i) in_place = in_place && a.out[i] == a.data[i];
-    by_tables(a, total, [&](const Table& t) {
-        hipLaunchKernelGGL(k_scale<A>, dim3(t.groups), dim3(NT), 0, s, t, part, groups, a.limit, in_place,
-                           norm);
-        norm = nullptr;
-    });
+    const bool stream = units > kSmall;
+    if (in_place) scale<A, Inputs>(a, part, groups, stream, s);
+    else scale<A, Copies>(a, part, groups, stream, s);
     return true;
 }
 
 }  // namespace
 
 size_t grad_norm_workspace() {
-    return (kGroups + (HBSJD_GRAD_MAX_TENSORS + kTable - 1) / kTable) * sizeof(Squares);
+    static_assert(sizeof(Inputs) <= 4000 && sizeof(Copies) <= 4000, "arguments of a launch");
+    static_assert((HBSJD_GRAD_MAX_TENSORS + Inputs::kTensors - 1) / Inputs::kTensors <= kPartials, "");
+    return kPartials * sizeof(Squares);
 }
 
 bool grad_norm(const GradArgs& a, void* workspace, hipStream_t s) {
