@@ -350,6 +350,7 @@ struct TokenArgs {
     float2 log2_tau;               // log2 e / temperature in two parts
     void* grad;                    // [rows], stride ld_grad, or null
     int64_t ld_grad;
+    bool stream;                   // rows and gradients are past what the caches hold
     float* logprob;                // [rows] or null
     float* entropy;                // [rows] or null
     // the loss is a sum of l and H with these weights...

@@ -4,11 +4,13 @@
 // With p = softmax(z / tau) of a row, y its token, l = log p_y and H = -sum p log p:
 //   dl/dz_v = (1[v = y] - p_v) / tau,   dH/dz_v = -p_v (log p_v + H) / tau.
 // All losses here reach the logits through the two slopes g = dL/dl and h = dL/dH.
-// With m the row's largest logit, d_v = z_v - m, e_v = exp(d_v / tau), s = sum e
-// and T = sum e d, H - log s = -T / (tau s), and the gradient is
-//   e_v (A_0 + A_1 d_v),   A_0 = -(g - h T / (tau s)) / (tau s),   A_1 = -h / (tau^2 s)
+// An entry's exponential is e_v = 2^x_v, x_v = z_v c - k with c = log2 e / tau and k
+// next to the largest z c: one fused operation ahead of the hardware's exp2. k is a
+// rounded number, and what it is off by is put back in 64 bits. With s = sum e and
+// X = sum e x / s, log p_v = x_v ln 2 - log s, H = log s - X ln 2, and the gradient is
+//   e_v (A_0 + A_1 x_v),   A_0 = -(g - h X ln 2) / (tau s),   A_1 = -h ln 2 / (tau s)
 // away from the token, and at it
-//   (g s_o / s - h e_y (d_y - T / s) / (tau s)) / tau,
+//   (g s_o / s - h p_y (l + H)) / tau,
 // s_o the sum over all entries but the token's. That sum is formed by itself: for a
 // token that is nearly certain, 1 - p_y = s_o / s and l = -log(1 + s_o / e_y) would
 // be differences of almost equal numbers.
@@ -26,9 +28,71 @@ namespace {
 // exponents (to base 2) below this give an e_v of 0 in any case
 constexpr float kFar = -200.f;
 
+// How a row's exponents are formed: as above, or (logits so large, or a temperature so
+// small, that z c has no digits left behind the binary point, and rows without a largest
+// logit) with the entries replaced by z - m first, and k = 0. Of two entries of such a
+// row whose exponents differ by less than 200, z - m is exact in fp32; in 16 bits there
+// are none but equal ones.
+struct Exponents {
+    float c, k;
+    double off;   // what k falls short of m c by, in nats: exponents are that much too large
+    bool near;
+
+    __device__ __forceinline__ static Exponents of(float m, float2 c2) {
+        Exponents x;
+        x.c = c2.x + c2.y;   // to nearest
+        x.k = m * x.c;
+        x.near = fabsf(x.k) < 1048576.f;
+        x.off = fma((double)m, (double)x.c, -(double)x.k) * 0.6931471805599453094;
+        if (!x.near) {
+            x.k = 0.f;
+            x.off = 0.0;
+        }
+        return x;
+    }
+    __device__ __forceinline__ float at(float z) const { return fmaf(z, c, -k); }
+};
+
 // What the entries of a row or a part come to.
 struct Sums {
-    double s = 0.0, t = 0.0;   // without the token's entry
+    double s = 0.0, t = 0.0;   // sums of e and e x, without the token's entry
+};
+
+// the largest entry of a vector, and m; a NaN counts for nothing, and a bf16 infinity
+// may not either (the sum is none then)
+template <typename T> struct Largest {
+    float m = -INFINITY;
+    __device__ __forceinline__ void add(const u32x4& v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m = fmaxf(m, __uint_as_float(v[q]));
+    }
+    __device__ __forceinline__ float get() const { return m; }
+};
+// as pairs: an upper entry as the float that its pair is, whose other digits change no
+// order between different ones
+template <> struct Largest<Bf16> {
+    float lo = -INFINITY, hi = -INFINITY;
+    __device__ __forceinline__ void add(const u32x4& v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            lo = fmaxf(lo, __uint_as_float(v[q] << 16));
+            hi = fmaxf(hi, __uint_as_float(v[q]));
+        }
+    }
+    __device__ __forceinline__ float get() const {
+        return fmaxf(lo, __uint_as_float(__float_as_uint(hi) & 0xFFFF0000u));
+    }
+};
+template <> struct Largest<F16> {
+    f16x2 m = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+    __device__ __forceinline__ void add(const u32x4& v) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t pair = v[q];
+            m = __builtin_elementwise_max(m, __builtin_bit_cast(f16x2, pair));
+        }
+    }
+    __device__ __forceinline__ float get() const { return fmaxf((float)m[0], (float)m[1]); }
 };
 
 template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
@@ -38,6 +102,19 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
     using RowRegs<T, NT, NV>::sp;
     int jy, qy, ey;   // the token's vector and place in it, or its edge; -1: elsewhere
 
+    // stream: the row is not looked for in the caches again
+    __device__ __forceinline__ void load(const T* z, int V, bool stream) {
+        if (!stream) return RowRegs<T, NT, NV>::load(z, V);
+        sp = Span::of(z, V);
+        xe = -INFINITY;
+        const u32x4* z4 = (const u32x4*)(z + sp.head);
+        if (sp.vecs > 0)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                x[i] = __builtin_nontemporal_load(&vec_at(z4, min((int)threadIdx.x + NT * i, sp.vecs - 1)));
+        if ((int)threadIdx.x < sp.edges()) xe = widen(z[sp.edge(threadIdx.x, V)]);
+        asm volatile("");   // else the compiler makes one of the two, with usual loads
+    }
     // y: the token's entry relative to this row or part
     __device__ __forceinline__ void find(int y, int V) {
         jy = ey = -1;
@@ -51,60 +128,73 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
             qy = p % E;
         }
     }
+    // z - m in place of z
+    __device__ __forceinline__ void recenter(float m) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float y[E];
+#pragma unroll
+            for (int q = 0; q < E; ++q) y[q] = vec_get<T>(x[i], q) - m;
+            x[i] = vec_pack<T>(y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        xe -= m;
+    }
+    // else the compiler keeps entries that a pass has unpacked for the next one
+    __device__ __forceinline__ void keep_packed() {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
+    }
     // The token's entry and what lies behind the row become -infinity. Returns the
     // largest of the rest.
     __device__ __forceinline__ float largest() {
-        float m = -INFINITY;
+        Largest<T> m;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = threadIdx.x + NT * i;
             if (j >= sp.vecs) {
                 x[i] = masked_vec<T>();
-                continue;
-            }
-            if (j == jy)
+            } else if (j == jy) {
 #pragma unroll
                 for (int q = 0; q < E; ++q) vec_mask<T>(x[i], q, q == qy);
-#pragma unroll
-            for (int q = 0; q < E; ++q) m = fmaxf(m, vec_get<T>(x[i], q));
+            }
+            m.add(x[i]);
             __builtin_amdgcn_sched_barrier(0);
         }
         if ((int)threadIdx.x == ey) xe = -INFINITY;
-        return fmaxf(m, xe);
+        keep_packed();
+        return fmaxf(m.get(), xe);
     }
     template <bool Ent>
-    __device__ __forceinline__ void add(float d, float2 c2, float far, float& s, float& t) {
-        const float e = power(d, c2);
+    __device__ __forceinline__ void add(float z, const Exponents& ex, float& s, float& t) const {
+        const float y = ex.at(z), e = __builtin_amdgcn_exp2f(y);
         s += e;
-        if constexpr (Ent) t = fmaf(e, fmaxf(d, far), t);
+        if constexpr (Ent) t = fmaf(e, fmaxf(y, kFar), t);
     }
-    // this thread's part of s and T
-    template <bool Ent> __device__ __forceinline__ Sums sum(float m, float2 c2, float far) {
+    // this thread's part of the sums
+    template <bool Ent> __device__ __forceinline__ Sums sum(const Exponents& ex) {
         float s = 0.f, t = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float sv = 0.f, tv = 0.f;   // a vector's own sums: shorter chains of roundings
 #pragma unroll
-            for (int q = 0; q < E; ++q) add<Ent>(vec_get<T>(x[i], q) - m, c2, far, sv, tv);
+            for (int q = 0; q < E; ++q) add<Ent>(vec_get<T>(x[i], q), ex, sv, tv);
             s += sv;
             t += tv;
             __builtin_amdgcn_sched_barrier(0);
         }
-        add<Ent>(xe - m, c2, far, s, t);
+        add<Ent>(xe, ex, s, t);
         return Sums{(double)s, (double)t};
     }
     template <bool Ent>
-    __device__ __forceinline__ static float value(float d, float2 c2, float far, float a0, float a1) {
-        // 16-bit gradients: what log2 e / tau loses as one number lies below their rounding
-        const float e = E == 4 ? power(d, c2) : __builtin_amdgcn_exp2f(d * c2.x);
-        return Ent ? e * fmaf(a1, fmaxf(d, far), a0) : e * a0;
+    __device__ __forceinline__ static float value(float z, const Exponents& ex, float a0, float a1) {
+        const float y = ex.at(z), e = __builtin_amdgcn_exp2f(y);
+        return Ent ? e * fmaf(a1, fmaxf(y, kFar), a0) : e * a0;
     }
-    // the gradient, after largest(); gy: at the token
+    // the gradient; gy: at the token
     template <bool Ent>
-    __device__ __forceinline__ void store(T* g, const T* z, int V, float m, float2 c2, float far, float a0,
+    __device__ __forceinline__ void store(T* g, const T* z, int V, bool stream, const Exponents& ex, float a0,
                                           float a1, float gy) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(x[i]));
         const bool same = (((uintptr_t)g ^ (uintptr_t)z) & 15) == 0;
         T* gv = g + sp.head;
 #pragma unroll
@@ -112,21 +202,27 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
             const int j = threadIdx.x + NT * i;
             float y[E];
 #pragma unroll
-            for (int q = 0; q < E; ++q) y[q] = value<Ent>(vec_get<T>(x[i], q) - m, c2, far, a0, a1);
+            for (int q = 0; q < E; ++q) y[q] = value<Ent>(vec_get<T>(x[i], q), ex, a0, a1);
             if (j == jy)
 #pragma unroll
                 for (int q = 0; q < E; ++q) y[q] = q == qy ? gy : y[q];
             __builtin_amdgcn_sched_barrier(0);
             if (j >= sp.vecs) continue;
             if (same) {
-                vec_at((u32x4*)gv, j) = vec_pack<T>(y);
+                if (stream) {
+                    asm volatile("");   // (as above)
+                    __builtin_nontemporal_store(vec_pack<T>(y), &vec_at((u32x4*)gv, j));
+                    asm volatile("");
+                } else {
+                    vec_at((u32x4*)gv, j) = vec_pack<T>(y);
+                }
             } else {
 #pragma unroll
                 for (int q = 0; q < E; ++q) gv[j * E + q] = narrow<T>(y[q]);
             }
         }
         if ((int)threadIdx.x < sp.edges()) {
-            const float ye = value<Ent>(xe - m, c2, far, a0, a1);
+            const float ye = value<Ent>(xe, ex, a0, a1);
             g[sp.edge(threadIdx.x, V)] = narrow<T>((int)threadIdx.x == ey ? gy : ye);
         }
     }
@@ -134,23 +230,39 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
 
 // ---- a row's results from its sums
 
+constexpr double kLn2d = 0.6931471805599453094;
+
 struct RowEnd {
-    double l, entropy, s, se, t;   // s: all of the row; se: without the token; t: all
-    double ey, dy;
+    double l, entropy;
+    double s, se, ey;   // sums of e: the row's, without the token, the token's
+    double xy, mean;    // the token's exponent and the mean of all, in nats
 };
 
-// m: the largest logit, zy: the token's
-__device__ __forceinline__ RowEnd row_end(float m, float zy, Sums o, double inv_tau) {
+// a condition; One: every lane of the wavefront has the same
+template <bool One> __device__ __forceinline__ bool holds(bool x) {
+    if constexpr (One) return uniform((int)x) != 0;
+    return x;
+}
+
+// m: the largest logit, zy: the token's, o: the sums with the exponents ex. One: the
+// wavefront works on one row, else every lane on its own
+template <bool One>
+__device__ __forceinline__ RowEnd row_end(float m, float zy, Sums o, double off, double inv_tau) {
     RowEnd r;
-    r.dy = (double)zy - (double)m;
-    const double x = r.dy * inv_tau;
-    r.ey = exp_of(x);
+    const double x = ((double)zy - (double)m) * inv_tau;
+    r.xy = x + off;
+    r.ey = exp_of(r.xy);
     r.se = o.s;
     r.s = o.s + r.ey;
-    r.t = r.ey > 0.0 ? o.t + r.ey * r.dy : o.t;
-    r.l = r.ey >= o.s ? -log1p(o.s / r.ey) : x - log(r.s);
-    r.entropy = (r.ey >= o.s ? x - r.l : log(r.s)) - r.t * inv_tau / r.s;
-    // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or NaN)
+    // a token that has most of the mass is the largest entry: x is 0
+    const bool most = holds<One>(r.ey >= o.s);
+    double up;
+    if (most) up = log1p(o.s / r.ey);
+    else up = log(r.s);
+    r.l = most ? -up : r.xy - up;
+    r.mean = (o.t * kLn2d + (r.ey > 0.0 ? r.ey * r.xy : 0.0)) / r.s;
+    r.entropy = (most ? up + r.xy : up) - r.mean;
+    // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or none)
     if (!(r.s > 0.0 && r.s < INFINITY)) r.l = r.entropy = (double)kNan;
     return r;
 }
@@ -169,7 +281,8 @@ __device__ __forceinline__ Goal goal_of(const TokenArgs& a, int64_t r, double l,
         return o;
     }
     const double adv = a.advantage[r];
-    const double rho = a.old_logprob ? exp(l - (double)a.old_logprob[r]) : l == l ? 1.0 : l;
+    double rho = l == l ? 1.0 : l;
+    if (a.old_logprob) rho = exp(l - (double)a.old_logprob[r]);
     const double bound = adv > 0.0 ? a.high : a.low;
     const bool beyond = adv > 0.0 ? rho > bound : rho < bound;
     if (adv != 0.0) {   // (a NaN is taken along)
@@ -199,12 +312,11 @@ struct Slopes {
     bool ok;
 };
 __device__ __forceinline__ Slopes slopes_of(const RowEnd& e, const Goal& o, double inv_tau) {
-    const double f = inv_tau / e.s, mean = e.t / e.s;   // of d
+    const double f = inv_tau / e.s;
     Slopes s;
-    s.a0 = (float)(-f * (o.g - o.h * mean * inv_tau));
-    s.a1 = (float)(-f * o.h * inv_tau);
-    const double py_d = e.ey > 0.0 ? e.ey * (e.dy - mean) : 0.0;
-    s.gy = (float)(f * (o.g * e.se - o.h * py_d * inv_tau));
+    s.a0 = (float)(-f * (o.g - o.h * e.mean));
+    s.a1 = (float)(-f * o.h * kLn2d);
+    s.gy = (float)(f * (o.g * e.se - (e.ey > 0.0 ? o.h * e.ey * (e.xy - e.mean) : 0.0)));
     return s;
 }
 
@@ -230,10 +342,13 @@ __device__ __forceinline__ void no_number(const TokenArgs& a, int64_t r, T* g, i
 
 // One wavefront works a row out in 64 bits and leaves the slopes in `shared`
 // (every wavefront doing so would take as long as the exponentials).
-__device__ __forceinline__ void finish(const TokenArgs& a, int64_t r, float m, float zy, Sums o, float w,
-                                       bool first, Slopes* shared) {
-    const RowEnd e = row_end(m, zy, o, a.inv_tau);
+__device__ __forceinline__ void finish(const TokenArgs& a, int64_t r, float m, float zy, Sums o, double off,
+                                       float w, bool first, Slopes* shared) {
+    // one after the other: the row's registers leave little room
+    const RowEnd e = row_end<true>(m, zy, o, off, a.inv_tau);
+    __builtin_amdgcn_sched_barrier(0);
     const Goal goal = goal_of(a, r, e.l, e.entropy, w);
+    __builtin_amdgcn_sched_barrier(0);
     Slopes s = slopes_of(e, goal, a.inv_tau);
     // a loss without an end leaves no gradient; a log-probability of -infinity does
     const float loss = (float)goal.loss;
@@ -248,39 +363,39 @@ __device__ __forceinline__ void finish(const TokenArgs& a, int64_t r, float m, f
     }
 }
 
-__device__ __forceinline__ float far_of(const TokenArgs& a) { return kFar / a.log2_tau.x; }
-
-// A workgroup of NT threads a row.
-template <typename T, int NT, int NV, bool Ent>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_token(
+// A workgroup of NT threads a row. (With a gradient four wavefronts a SIMD are what the
+// rows in flight leave, see resident_lds().)
+template <typename T, int NT, int NV, bool Ent, bool Grad>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(Grad ? 4 : waves_of(NT)))) void k_token(
     TokenArgs a, int64_t r0) {
     __shared__ float red[NT / 64];
     __shared__ double red2[2][NT / 64];
     __shared__ Slopes shared;
     const int64_t r = r0 + blockIdx.x;
     const T* z = (const T*)a.logits + r * a.ld;
-    T* g = a.grad ? (T*)a.grad + r * a.ld_grad : nullptr;
+    T* g = Grad ? (T*)a.grad + r * a.ld_grad : nullptr;
     const int y = a.tokens[r];
     const float w = a.weight ? a.weight[r] : 1.f;
     if (y == -1 || w == 0.f) return no_part<NT>(a, r, g, a.V, true);
     if (y < 0 || y >= a.V) return no_number<NT>(a, r, g, a.V, true);
     TokenRow<T, NT, NV> row;
-    row.load(z, a.V);
+    row.load(z, a.V, a.stream);
     const float zy = widen(z[y]);
     row.find(y, a.V);
-    float m = block_all<NT>(row.largest(), red, MaxOp());
-    m = fmaxf(m, zy);
-    const float2 c2 = a.log2_tau;
-    const float far = far_of(a);
-    const Sums o = row.template sum<Ent>(m, c2, far);
+    const float m = fmaxf(block_all<NT>(row.largest(), red, MaxOp()), zy);
+    const Exponents ex = Exponents::of(uniform(m), a.log2_tau);
+    if (!ex.near) row.recenter(m);
+    const Sums o = row.template sum<Ent>(ex);
     double s[2] = {o.s, o.t};
     block_all<NT, Ent ? 2 : 1>(*(double(*)[Ent ? 2 : 1])s, red2, AddOp());
-    if (threadIdx.x < 64) finish(a, r, m, zy, Sums{s[0], s[1]}, w, true, &shared);
-    if (!g) return;
+    if (threadIdx.x < 64) finish(a, r, m, zy, Sums{s[0], s[1]}, ex.off, w, true, &shared);
+    if constexpr (!Grad) return;
     __syncthreads();
     const Slopes sl = shared;
     if (!sl.ok) return fill_row<NT>(g, a.V, kNan);
-    row.template store<Ent>(g, z, a.V, m, c2, far, uniform(sl.a0), uniform(sl.a1), uniform(sl.gy));
+    const float a0 = uniform(sl.a0), a1 = uniform(sl.a1), gy = uniform(sl.gy);
+    row.keep_packed();
+    row.template store<Ent>(g, z, a.V, a.stream, ex, a0, a1, gy);
 }
 
 // ---- rows in parts
@@ -297,30 +412,36 @@ struct PartsArgs {
 // the sums of a part, or of a whole row where parts = 1
 template <typename T, int NT, int NV, bool Ent>
 __device__ __forceinline__ void part_stats(const TokenArgs& a, const PartsArgs& p, int64_t r, int c, int y,
-                                           PartStats* out) {
+                                           PartStats* out, bool stream) {
     __shared__ float red[NT / 64];
     __shared__ double red2[2][NT / 64];
     const int first = c * p.len, V = min(p.len, a.V - first);
     const T* z = (const T*)a.logits + r * a.ld + first;
     TokenRow<T, NT, NV> row;
-    row.load(z, V);
+    row.load(z, V, stream);
     const bool here = y >= first && y < first + V;
     const float zy = here ? widen(z[y - first]) : 0.f;
     row.find(y - first, V);
     const float m = block_all<NT>(row.largest(), red, MaxOp());
     // relative to a finite number: a part of -infinities sums to 0
-    const Sums o = row.template sum<Ent>(m == -INFINITY ? 0.f : m, a.log2_tau, far_of(a));
+    const float from = m == -INFINITY ? 0.f : m;
+    const Exponents ex = Exponents::of(from, a.log2_tau);
+    if (!ex.near) row.recenter(from);
+    const Sums o = row.template sum<Ent>(ex);
     double s[2] = {o.s, o.t};
     block_all<NT, Ent ? 2 : 1>(*(double(*)[Ent ? 2 : 1])s, red2, AddOp());
     if (threadIdx.x == 0) *out = PartStats{m, (float)s[0], Ent ? (float)s[1] : 0.f, zy};
 }
 
-// The sums of a part relative to the row's largest logit.
+// The sums of a part with the exponents of its row.
 template <bool Ent>
-__device__ __forceinline__ Sums part_sums(const PartStats& q, float m, float2 c2, float far) {
+__device__ __forceinline__ Sums part_sums(const PartStats& q, float m, const Exponents& ex, float2 c2,
+                                          double inv_tau) {
     if (q.m == -INFINITY) return Sums{(double)q.s, 0.0};
-    const float d = q.m - m, e = power(d, c2);
-    return Sums{(double)q.s * e, Ent ? ((double)q.t + (double)q.s * fmaxf(d, far)) * e : 0.0};
+    // what the part's exponents are off by in the row, to base 2
+    const double by = (((double)q.m - (double)m) * inv_tau + ex.off - Exponents::of(q.m, c2).off) / kLn2d;
+    const float e = exp_of(by * kLn2d);
+    return Sums{(double)q.s * e, Ent && e > 0.f ? ((double)q.t + (double)q.s * by) * e : 0.0};
 }
 
 template <typename T, int NT, int NV, bool Ent>
@@ -330,7 +451,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     const int64_t r = r0 + row;
     const int y = a.tokens[r];
     if (y < 0 || y >= a.V || (a.weight && a.weight[r] == 0.f)) return;
-    part_stats<T, NT, NV, Ent>(a, p, r, c, y, p.stats + (int64_t)row * p.parts + c);
+    part_stats<T, NT, NV, Ent>(a, p, r, c, y, p.stats + (int64_t)row * p.parts + c, false);
 }
 
 // Joins a row's parts (every part's workgroup does, a lane a part) and stores the
@@ -349,28 +470,30 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     if (y == -1 || w == 0.f) return no_part<NT>(a, r, g, V, c == 0);
     if (y < 0 || y >= a.V) return no_number<NT>(a, r, g, V, c == 0);
     TokenRow<T, NT, NV> part;
-    if (g) part.load(z, V);
+    if (g) part.load(z, V, a.stream);
     else if (c > 0) return;   // without a gradient one workgroup a row is enough
     const PartStats* stats = p.stats + (int64_t)row * p.parts;
     const int lane = threadIdx.x & 63;
     const float2 c2 = a.log2_tau;
-    const float far = far_of(a), zy = stats[y / p.len].zy;
+    const float zy = stats[y / p.len].zy;
     PartStats q{-INFINITY, 0.f, 0.f, 0.f};
     if (lane < p.parts) q = stats[lane];
     const float m = fmaxf(wave_all(q.m, MaxOp()), zy);
+    const Exponents ex = Exponents::of(m, c2);
     if (threadIdx.x < 64) {
-        Sums o = part_sums<Ent>(q, m, c2, far);
+        Sums o = part_sums<Ent>(q, m, ex, c2, a.inv_tau);
         o.s = wave_all(o.s, AddOp());
         if constexpr (Ent) o.t = wave_all(o.t, AddOp());
-        finish(a, r, m, zy, o, w, c == 0, &shared);
+        finish(a, r, m, zy, o, ex.off, w, c == 0, &shared);
     }
     if (!g) return;
     __syncthreads();
     const Slopes sl = shared;
     if (!sl.ok) return fill_row<NT>(g, V, kNan);
     part.find(y - first, V);
-    part.largest();
-    part.template store<Ent>(g, z, V, m, c2, far, uniform(sl.a0), uniform(sl.a1), uniform(sl.gy));
+    const float a0 = uniform(sl.a0), a1 = uniform(sl.a1), gy = uniform(sl.gy);
+    if (!ex.near) part.recenter(m);
+    part.template store<Ent>(g, z, V, a.stream, ex, a0, a1, gy);
 }
 
 // ---- pairs of sequences
@@ -383,6 +506,7 @@ struct RowSlope {
 struct PairArgs {
     PartsArgs p;
     RowSlope* slope;   // [rows]
+    int64_t streams;   // rows that the second reading will not find in the caches
 };
 
 // the first reading: a row's sums
@@ -396,7 +520,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     const bool in = !q.first || (r >= q.first[0] && r < q.first[2 * q.pairs]);
     if (c == 0 && threadIdx.x == 0) b.slope[r] = RowSlope{0.f, 0.f, 0.f, 0};
     if (!in || y < 0 || y >= a.V) return;
-    part_stats<T, NT, NV, false>(a, b.p, r, c, y, b.p.stats + r * b.p.parts + c);
+    part_stats<T, NT, NV, false>(a, b.p, r, c, y, b.p.stats + r * b.p.parts + c, r < b.streams);
 }
 
 constexpr int kPairThreads = 1024;
@@ -432,9 +556,10 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
             const float zy = stats[y / b.p.len].zy;
             o.m = zy;
             for (int c = 0; c < b.p.parts; ++c) o.m = fmaxf(o.m, stats[c].m);
+            const Exponents ex = Exponents::of(o.m, c2);
             Sums sum;
-            for (int c = 0; c < b.p.parts; ++c) sum.s += part_sums<false>(stats[c], o.m, c2, 0.f).s;
-            const RowEnd e = row_end(o.m, zy, sum, a.inv_tau);
+            for (int c = 0; c < b.p.parts; ++c) sum.s += part_sums<false>(stats[c], o.m, ex, c2, a.inv_tau).s;
+            const RowEnd e = row_end<false>(o.m, zy, sum, ex.off, a.inv_tau);
             l = e.l;
             const Slopes sl = slopes_of(e, Goal{0.0, 1.0, 0.0}, a.inv_tau);
             o.a0 = sl.a0;
@@ -448,48 +573,54 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
         s[2 + which] += 1.0;
     }
     block_all<NT, 4>(s, red, AddOp());
-    double n[2] = {1.0, 1.0};
-    if (q.mean)
-        for (int i = 0; i < 2; ++i) n[i] = fmax(s[2 + i], 1.0);
-    const double chosen = bad ? (double)kNan : s[0] / n[0], rejected = bad ? (double)kNan : s[1] / n[1];
-    const double u = chosen - rejected - q.margin, h = q.beta * u;
-    double loss, slope;   // slope: by u
-    if (q.form == HBSJD_PREFERENCE_SIGMOID) {
-        loss = (1.0 - q.smoothing) * softplus(-h);
-        slope = -(1.0 - q.smoothing) * logistic(-h);
-        if (q.smoothing > 0.0) {
-            loss += q.smoothing * softplus(h);
-            slope += q.smoothing * logistic(h);
+    __shared__ double by_l[2];   // the loss's slopes by the two sequences' log-probabilities
+    __shared__ int sound;
+    if (threadIdx.x < 64) {      // every wavefront doing this would take 4 us
+        double n[2] = {1.0, 1.0};
+        if (q.mean)
+            for (int i = 0; i < 2; ++i) n[i] = fmax(s[2 + i], 1.0);
+        const double chosen = bad ? (double)kNan : s[0] / n[0], rejected = bad ? (double)kNan : s[1] / n[1];
+        const double u = chosen - rejected - q.margin, h = q.beta * u;
+        double loss, slope;   // slope: by u
+        if (q.form == HBSJD_PREFERENCE_SIGMOID) {
+            loss = (1.0 - q.smoothing) * softplus(-h);
+            slope = -(1.0 - q.smoothing) * logistic(-h);
+            if (q.smoothing > 0.0) {
+                loss += q.smoothing * softplus(h);
+                slope += q.smoothing * logistic(h);
+            }
+            slope *= q.beta;
+        } else if (q.form == HBSJD_PREFERENCE_HINGE) {
+            loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+            slope = h < 1.0 ? -q.beta : 0.0;
+        } else {
+            const double d = u - 0.5 / q.beta;
+            loss = d * d;
+            slope = 2.0 * d;
         }
-        slope *= q.beta;
-    } else if (q.form == HBSJD_PREFERENCE_HINGE) {
-        loss = h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
-        slope = h < 1.0 ? -q.beta : 0.0;
-    } else {
-        const double d = u - 0.5 / q.beta;
-        loss = d * d;
-        slope = 2.0 * d;
-    }
-    const float w = q.weight ? q.weight[pair] : 1.f;
-    const float value = w == 0.f ? 0.f : (float)(w * loss);
-    if (threadIdx.x == 0) {
-        if (q.loss) q.loss[pair] = value;
-        if (q.log_ratio) {
-            q.log_ratio[2 * pair] = (float)chosen;
-            q.log_ratio[2 * pair + 1] = (float)rejected;
+        const float w = q.weight ? q.weight[pair] : 1.f;
+        const float value = w == 0.f ? 0.f : (float)(w * loss);
+        if (threadIdx.x == 0) {
+            if (q.loss) q.loss[pair] = value;
+            if (q.log_ratio) {
+                q.log_ratio[2 * pair] = (float)chosen;
+                q.log_ratio[2 * pair + 1] = (float)rejected;
+            }
+            sound = !bad && value > -INFINITY && value < INFINITY;
+            by_l[0] = w == 0.f ? 0.0 : w * slope / n[0];
+            by_l[1] = w == 0.f ? 0.0 : -w * slope / n[1];
         }
     }
     if (!a.grad) return;
-    const bool ok = value > -INFINITY && value < INFINITY;
-    const double by_l[2] = {w * slope / n[0], -w * slope / n[1]};
+    __syncthreads();
     for (int64_t r = at[0] + threadIdx.x; r < (bad ? max(at[1], at[2]) : at[2]); r += NT) {
         if (a.tokens[r] == -1) continue;
         RowSlope o{0.f, kNan, kNan, 1};
-        if (ok && !bad) {
+        if (sound) {
             o = b.slope[r];
             const double f = by_l[r >= at[1] ? 1 : 0];
-            o.a0 = w == 0.f || f == 0.0 ? 0.f : (float)(o.a0 * f);
-            o.gy = w == 0.f || f == 0.0 ? 0.f : (float)(o.gy * f);
+            o.a0 = f == 0.0 ? 0.f : (float)(o.a0 * f);   // (a row in error weighted out)
+            o.gy = f == 0.0 ? 0.f : (float)(o.gy * f);
         }
         b.slope[r] = o;
     }
@@ -509,9 +640,11 @@ __global__ __launch_bounds__(NT) void k_pair_grad(TokenArgs a, PairArgs b, int c
     if (!uniform(o.used) || (a0 == 0.f && gy == 0.f)) return fill_row<NT>(g, V, 0.f);
     if (a0 != a0 || gy != gy) return fill_row<NT>(g, V, kNan);
     TokenRow<T, NT, NV> part;
-    part.load(z, V);
+    part.load(z, V, a.stream);
     part.find(a.tokens[r] - first, V);
-    part.template store<false>(g, z, V, m, a.log2_tau, 0.f, a0, 0.f, gy);
+    const Exponents ex = Exponents::of(m, a.log2_tau);
+    if (!ex.near) part.recenter(m);
+    part.template store<false>(g, z, V, a.stream, ex, a0, 0.f, gy);
 }
 
 // ---- how a call runs
@@ -568,16 +701,31 @@ template <typename T, bool Ent> void go(const TokenArgs& a, void* ws, hipStream_
         }
         return;
     }
-    const size_t lds = a.grad ? resident_lds(0, a.V * sizeof(T)) : 0;
+    const size_t lds = resident_lds(0, a.V * sizeof(T));
     by_size<T>(a.V, [&](auto nt, auto nv) {
         by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-            hipLaunchKernelGGL((k_token<T, decltype(nt)::value, decltype(nv)::value, Ent>), grid,
-                               dim3(decltype(nt)::value), lds, s, a, r0);
+            constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
+            if (a.grad) hipLaunchKernelGGL((k_token<T, NT, NV, Ent, true>), grid, dim3(NT), lds, s, a, r0);
+            else hipLaunchKernelGGL((k_token<T, NT, NV, Ent, false>), grid, dim3(NT), 0, s, a, r0);
         });
     });
 }
 
-template <typename T> void go_token(const TokenArgs& a, void* ws, hipStream_t s) {
+// Calls on more than 64 MB read rows for the last time, and write gradients, as streams.
+// Passes among others, with usual loads and stores, with streamed stores, with both: log-
+// probabilities of 6144 fp32 rows of 16384 72, 72, 65 us; policy loss and gradient there
+// 147, 141, 142; gradients of 18432 bf16 rows 195, 191, 177; 8192 bf16 rows in pairs 132,
+// 121, 120; 4 pairs of 101 bf16 rows of 128257 104, 97, 89. (Of less, what reads the
+// gradient next finds it in the cache.)
+constexpr int64_t kSmall = 64 << 20, kCached = 192 << 20;
+template <typename T> TokenArgs streamed(const TokenArgs& a) {
+    TokenArgs b = a;
+    b.stream = a.rows * a.V * (int64_t)sizeof(T) > kSmall;
+    return b;
+}
+
+template <typename T> void go_token(const TokenArgs& args, void* ws, hipStream_t s) {
+    const TokenArgs a = streamed<T>(args);
     const bool entropy = a.entropy || a.entropy_weight || (a.advantage && a.bonus > 0.f);
     if (entropy) go<T, true>(a, ws, s);
     else go<T, false>(a, ws, s);
@@ -592,16 +740,20 @@ Plan pair_plan(int64_t rows, int V) {
 // workgroups of the second reading take 256 KB / 16 = 16 KB of a row
 template <typename T> constexpr int kChunk2 = 256 * 4 * kVec<T>;
 
-template <typename T> void go_pairs(const TokenArgs& a, const PreferenceArgs& q, void* ws, hipStream_t s) {
+template <typename T>
+void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStream_t s) {
+    const TokenArgs a = streamed<T>(args);
     const Plan plan = pair_plan(a.rows, a.V);
     PairArgs b;
     b.slope = (RowSlope*)ws;
+    b.streams = std::max<int64_t>(0, a.rows - kCached / (int64_t)(a.V * sizeof(T)));
     b.p = PartsArgs{plan.parts, plan.len, (PartStats*)(b.slope + a.rows)};
+    const size_t lds = resident_lds(0, plan.len * sizeof(T));
     by_size<T>(plan.len, [&](auto nt, auto nv) {
         constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
         if constexpr (NT <= 512)   // a part's entries are no more
             by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
-                hipLaunchKernelGGL((k_pair_stats<T, NT, NV>), grid, dim3(NT), 0, s, a, q, b, r0);
+                hipLaunchKernelGGL((k_pair_stats<T, NT, NV>), grid, dim3(NT), lds, s, a, q, b, r0);
             }, plan.parts);
     });
     by_slabs(q.pairs, [&](int64_t p0, dim3 grid) {
