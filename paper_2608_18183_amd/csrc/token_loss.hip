@@ -136,6 +136,7 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
 #pragma unroll
             for (int q = 0; q < E; ++q) y[q] = vec_get<T>(x[i], q) - m;
             x[i] = vec_pack<T>(y);
+            asm volatile("" : "+v"(x[i]));   // (as below)
             __builtin_amdgcn_sched_barrier(0);
         }
         xe -= m;
@@ -178,7 +179,11 @@ template <typename T, int NT, int NV> struct TokenRow : RowRegs<T, NT, NV> {
         for (int i = 0; i < NV; ++i) {
             float sv = 0.f, tv = 0.f;   // a vector's own sums: shorter chains of roundings
 #pragma unroll
-            for (int q = 0; q < E; ++q) add<Ent>(vec_get<T>(x[i], q), ex, sv, tv);
+            for (int q = 0; q < E; ++q) {
+                add<Ent>(vec_get<T>(x[i], q), ex, sv, tv);
+                // else the compiler unpacks bf16 vectors ahead, and spills
+                if constexpr (Ent) asm volatile("" : "+v"(sv), "+v"(tv));
+            }
             s += sv;
             t += tv;
             __builtin_amdgcn_sched_barrier(0);
@@ -455,23 +460,22 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
 }
 
 // Joins a row's parts (every part's workgroup does, a lane a part) and stores the
-// gradient, reading the part again.
-template <typename T, int NT, int NV, bool Ent>
+// gradient, reading the part again. Without a gradient: a wavefront a row.
+template <typename T, int NT, int NV, bool Ent, bool Grad>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_token_rest(
     TokenArgs a, PartsArgs p, int64_t r0) {
     __shared__ Slopes shared;
-    const int row = blockIdx.x / p.parts, c = blockIdx.x - row * p.parts;
+    const int row = Grad ? blockIdx.x / p.parts : blockIdx.x, c = Grad ? blockIdx.x - row * p.parts : 0;
     const int64_t r = r0 + row;
     const int first = c * p.len, V = min(p.len, a.V - first);
     const T* z = (const T*)a.logits + r * a.ld + first;
-    T* g = a.grad ? (T*)a.grad + r * a.ld_grad + first : nullptr;
+    T* g = Grad ? (T*)a.grad + r * a.ld_grad + first : nullptr;
     const int y = a.tokens[r];
     const float w = a.weight ? a.weight[r] : 1.f;
     if (y == -1 || w == 0.f) return no_part<NT>(a, r, g, V, c == 0);
     if (y < 0 || y >= a.V) return no_number<NT>(a, r, g, V, c == 0);
     TokenRow<T, NT, NV> part;
-    if (g) part.load(z, V, a.stream);
-    else if (c > 0) return;   // without a gradient one workgroup a row is enough
+    if constexpr (Grad) part.load(z, V, a.stream);
     const PartStats* stats = p.stats + (int64_t)row * p.parts;
     const int lane = threadIdx.x & 63;
     const float2 c2 = a.log2_tau;
@@ -486,7 +490,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
         if constexpr (Ent) o.t = wave_all(o.t, AddOp());
         finish(a, r, m, zy, o, ex.off, w, c == 0, &shared);
     }
-    if (!g) return;
+    if constexpr (!Grad) return;
     __syncthreads();
     const Slopes sl = shared;
     if (!sl.ok) return fill_row<NT>(g, V, kNan);
@@ -664,17 +668,22 @@ void cut(Plan& p, int64_t rows, int V) {
     p.parts = (V + p.len - 1) / p.len;
 }
 
+// Parts where a workgroup cannot hold the row, and for rows above 128 KB that are few:
+// those of 65536 fp32 entries and fewer are held from 112 of them on. (900 fp32 rows of
+// 60000 with their gradients: held 95 us, in parts 111; 1000 bf16 rows of 100000, 128
+// registers of row and the arithmetic's on top: 198 held, spilling, 109 in parts.)
 Plan plan_of(int64_t rows, int V, int32_t elem) {
     Plan p;
-    const int64_t size = elem_size(elem);
-    const int64_t held = 1024 * 16 * (16 / size);
-    if (V * size <= 128 << 10 || (V <= held && rows >= 112)) return p;
+    if (V * (int64_t)elem_size(elem) <= 128 << 10 || (V <= 65536 && rows >= 112)) return p;
     cut(p, rows, V);
     p.slab = std::min<int64_t>(rows, (1 << 20) / p.parts);
     return p;
 }
 
-// f(threads, vectors a thread) of the workgroups that hold rows of V entries
+// f(threads, vectors a thread) of the workgroups that hold rows of V entries. (Two
+// workgroups of 512 threads and 16 vectors a CU, whose loads and stores overlap, for
+// rows of 64 to 128 KB: 1000 fp32 rows of 30000 45 us, one of 1024 threads and 8 vectors
+// 54; 3000 of 20000 92 and 122.)
 template <typename T, typename F> void by_size(int V, F f) {
     using std::integral_constant;
     const int vecs = V / kVec<T>;
@@ -684,7 +693,7 @@ template <typename T, typename F> void by_size(int V, F f) {
     else if (vecs <= 256 * 4) HELD(256, 4);
     else if (vecs <= 256 * 8) HELD(256, 8);
     else if (vecs <= 512 * 8) HELD(512, 8);
-    else if (vecs <= 1024 * 8) HELD(1024, 8);
+    else if (vecs <= 512 * 16) HELD(512, 16);
     else HELD(1024, 16);
 #undef HELD
 }
@@ -695,9 +704,10 @@ template <typename T, bool Ent> void go(const TokenArgs& a, void* ws, hipStream_
         constexpr int NT = 512, NV = kPart / kVec<T> / NT;
         const PartsArgs p{plan.parts, plan.len, (PartStats*)ws};
         for (int64_t r0 = 0; r0 < a.rows; r0 += plan.slab) {
-            const dim3 grid((unsigned)(std::min(plan.slab, a.rows - r0) * p.parts));
+            const dim3 rows((unsigned)std::min(plan.slab, a.rows - r0)), grid(rows.x * p.parts);
             hipLaunchKernelGGL((k_token_part<T, NT, NV, Ent>), grid, dim3(NT), 0, s, a, p, r0);
-            hipLaunchKernelGGL((k_token_rest<T, NT, NV, Ent>), grid, dim3(NT), 0, s, a, p, r0);
+            if (a.grad) hipLaunchKernelGGL((k_token_rest<T, NT, NV, Ent, true>), grid, dim3(NT), 0, s, a, p, r0);
+            else hipLaunchKernelGGL((k_token_rest<T, 64, 1, Ent, false>), rows, dim3(64), 0, s, a, p, r0);
         }
         return;
     }
@@ -751,7 +761,7 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
     const size_t lds = resident_lds(0, plan.len * sizeof(T));
     by_size<T>(plan.len, [&](auto nt, auto nv) {
         constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-        if constexpr (NT <= 512)   // a part's entries are no more
+        if constexpr (NT <= 512 && NV <= 8)   // a part's entries are no more
             by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
                 hipLaunchKernelGGL((k_pair_stats<T, NT, NV>), grid, dim3(NT), lds, s, a, q, b, r0);
             }, plan.parts);
