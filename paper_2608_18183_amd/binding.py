@@ -896,11 +896,12 @@ def _described(tensors, what: str, device):
     property takes 25 ns a tensor, the loop below ten times that.)"""
     T, types = _torch.Tensor, _ELEMS
     try:
-        at = array.array("Q", map(T.data_ptr, tensors))
-        sizes = array.array("q", map(T.numel, tensors))
+        at = array.array("Q", list(map(T.data_ptr, tensors)))
+        sizes = array.array("q", list(map(T.numel, tensors)))
         dtypes = list(map(_dtype_of, tensors))
         flat = all(map(T.is_contiguous, tensors))
-        sound = set(map(T.get_device, tensors)) <= {device.index} and types.keys() >= set(dtypes)
+        kinds = set(dtypes)
+        sound = set(map(T.get_device, tensors)) <= {device.index} and types.keys() >= kinds
     except (TypeError, RuntimeError, AttributeError, NotImplementedError):
         sound = flat = False
     if not sound or not flat:
@@ -911,7 +912,9 @@ def _described(tensors, what: str, device):
                 raise ValueError(f"{what}: fp32, bf16 or fp16, not {t.dtype}")
             if not _dense(t):
                 raise ValueError(f"{what}: a tensor's entries have to lie one after another")
-    return at, sizes, array.array("i", map(types.__getitem__, dtypes)), flat
+    if len(kinds) == 1:
+        return at, sizes, array.array("i", [types[dtypes[0]]]) * len(dtypes), flat
+    return at, sizes, array.array("i", [types[t] for t in dtypes]), flat
 
 
 def _start(a) -> int:

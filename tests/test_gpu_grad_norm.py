@@ -189,6 +189,27 @@ def test_more_entries_than_32_bits_count():
     assert int((x != 0).sum()) == 4
 
 
+def test_thousands_of_tensors():
+    """More than a launch, and than sixteen, describe; the last ones as the first."""
+    gen = torch.Generator("cuda").manual_seed(4)
+    flat = torch.randn(9000, generator=gen, device="cuda")
+    grads = [flat[3 * i:3 * i + 1 + i % 3] for i in range(3000)]
+    before = [g.clone() for g in (flat, *grads)]
+    want = norm64(grads, 2)
+    check_norm(P().hbsjd_grad_norm(grads), want)
+    check_norm(P().hbsjd_clip_grads(grads, want / 2), want)
+    scale = float(np.float32(want / 2)) / want
+    check_scaled(torch.cat(grads), torch.cat(before[1:]), scale)
+    out = [torch.empty_like(g) for g in grads]
+    P().hbsjd_clip_grads(grads, 0.0, out=out)
+    assert bool((torch.cat(out) == 0).all())
+    # what no tensor holds is as it was
+    held = torch.zeros(9000, dtype=torch.bool, device="cuda")
+    for i in range(3000):
+        held[3 * i:3 * i + 1 + i % 3] = True
+    assert torch.equal(flat[~held], before[0][~held])
+
+
 def test_captured_streams_and_the_same_bits():
     gen = torch.Generator("cuda").manual_seed(3)
     grads = [torch.randn(n, generator=gen, device="cuda").to(t)

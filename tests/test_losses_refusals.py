@@ -142,6 +142,14 @@ def test_clip_refuses(bad):
     assert _grads("clip", **bad) == "EINVAL"
 
 
+def test_grads_refuse_more_than_a_device_holds():
+    n = 200
+    big = dict(count=n, data=tuple(A + 16 * i for i in range(n)), sizes=((1 << 40) - 1,) * n, elems=(0,) * n)
+    assert _grads("norm", **big) == "EINVAL"
+    big["data"] = tuple(A + (i << 43) for i in range(n))
+    assert _grads("clip", **big) == "EINVAL"
+
+
 def test_grads_refuse_what_are_no_device_tensors():
     import torch
     for f in (lambda: P.hbsjd_grad_norm([torch.zeros(3)]), lambda: P.hbsjd_clip_grads([torch.zeros(3)], 1.0),
