@@ -668,13 +668,19 @@ void cut(Plan& p, int64_t rows, int V) {
     p.parts = (V + p.len - 1) / p.len;
 }
 
-// Parts where a workgroup cannot hold the row, and for rows above 128 KB that are few:
-// those of 65536 fp32 entries and fewer are held from 112 of them on. (900 fp32 rows of
-// 60000 with their gradients: held 95 us, in parts 111; 1000 bf16 rows of 100000, 128
-// registers of row and the arithmetic's on top: 198 held, spilling, 109 in parts.)
-Plan plan_of(int64_t rows, int V, int32_t elem) {
+// Rows above 128 KB go in parts, but for those of up to 256 KB that a workgroup holds, one
+// a CU: from 112 rows on (fewer leave CUs idle), with a gradient as long as the last
+// round of the 256 CUs is not mostly idle, without one where there is one round only. In
+// parts a gradient's rows are read twice, but reading alone has no need of registers:
+// policy loss and gradient, held and in parts, 900 fp32 rows of 60000 95 and 114 us, 1000
+// fp16 rows of 80000 81 and 86, 150 of 128257 26 and 29, but 300 bf16 ones of 70000 38
+// and 31; log-probabilities of 130 fp32 rows of 60000 9 and 15, of 900 49 and 36.
+Plan plan_of(int64_t rows, int V, int32_t elem, bool grad) {
     Plan p;
-    if (V * (int64_t)elem_size(elem) <= 128 << 10 || (V <= 65536 && rows >= 112)) return p;
+    const int64_t bytes = V * (int64_t)elem_size(elem);
+    const int64_t places = (rows + 255) / 256 * 256;
+    const bool filled = rows <= 256 || (grad && 4 * rows >= 3 * places);
+    if (bytes <= 128 << 10 || (bytes <= 256 << 10 && rows >= 112 && filled)) return p;
     cut(p, rows, V);
     p.slab = std::min<int64_t>(rows, (1 << 20) / p.parts);
     return p;
@@ -694,12 +700,13 @@ template <typename T, typename F> void by_size(int V, F f) {
     else if (vecs <= 256 * 8) HELD(256, 8);
     else if (vecs <= 512 * 8) HELD(512, 8);
     else if (vecs <= 512 * 16) HELD(512, 16);
+    else if (vecs <= 1024 * 12) HELD(1024, 12);
     else HELD(1024, 16);
 #undef HELD
 }
 
 template <typename T, bool Ent> void go(const TokenArgs& a, void* ws, hipStream_t s) {
-    const Plan plan = plan_of(a.rows, a.V, a.elem);
+    const Plan plan = plan_of(a.rows, a.V, a.elem, a.grad != nullptr);
     if (plan.parts) {
         constexpr int NT = 512, NV = kPart / kVec<T> / NT;
         const PartsArgs p{plan.parts, plan.len, (PartStats*)ws};
@@ -787,7 +794,7 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
 }  // namespace
 
 size_t token_workspace(int64_t rows, int V, int32_t elem) {
-    const Plan p = plan_of(rows, V, elem);
+    const Plan p = plan_of(rows, V, elem, false);   // where a gradient goes in parts, so does none
     return (size_t)p.slab * p.parts * sizeof(PartStats);
 }
 

@@ -577,6 +577,7 @@ def test_same_bits_alone_or_among_rows():
 
 
 @pytest.mark.parametrize("rows,V,dtype", [(6144, 16384, "f32"), (4608, 16384, "bf16"), (300, 60000, "f16"),
+                                          (300, 80001, "f16"), (420, 50001, "f32"),
                                           (130, 128257, "bf16"), (70000, 40, "f32"), (2_200_000, 3, "f16")])
 def test_batches(rows, V, dtype):
     """Batches of whole images, long and short rows, more rows than a launch takes:
