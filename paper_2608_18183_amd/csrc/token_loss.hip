@@ -513,6 +513,11 @@ struct PairArgs {
     int64_t streams;   // rows that the second reading will not find in the caches
 };
 
+// rows ahead of the first sequence and behind the last are left out
+__device__ __forceinline__ bool in_sequences(const PreferenceArgs& q, int64_t r) {
+    return !q.first || (r >= q.first[0] && r < q.first[2 * q.pairs]);
+}
+
 // the first reading: a row's sums
 template <typename T, int NT, int NV>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)))) void k_pair_stats(
@@ -520,8 +525,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     const int row = blockIdx.x / b.p.parts, c = blockIdx.x - row * b.p.parts;
     const int64_t r = r0 + row;
     const int y = a.tokens[r];
-    // rows ahead of the first sequence and behind the last are left out
-    const bool in = !q.first || (r >= q.first[0] && r < q.first[2 * q.pairs]);
+    const bool in = in_sequences(q, r);
     if (c == 0 && threadIdx.x == 0) b.slope[r] = RowSlope{0.f, 0.f, 0.f, 0};
     if (!in || y < 0 || y >= a.V) return;
     part_stats<T, NT, NV, false>(a, b.p, r, c, y, b.p.stats + r * b.p.parts + c, r < b.streams);
@@ -532,8 +536,50 @@ constexpr int kPairThreads = 1024;
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
 __device__ __forceinline__ double logistic(double x) { return 1.0 / (1.0 + exp(-x)); }
 
-// A workgroup a pair: its rows' log-probabilities, its loss, and the slope that
-// each of its rows takes from that.
+// l - ref of a row that has a token, from its parts; leaves the slopes of l
+__device__ __forceinline__ double row_ratio(const TokenArgs& a, const PreferenceArgs& q, const PairArgs& b,
+                                            int64_t r, int y) {
+    RowSlope o{0.f, kNan, kNan, 1};
+    double l = (double)kNan;
+    if (y >= 0 && y < a.V) {
+        const PartStats* stats = b.p.stats + r * b.p.parts;
+        const float zy = stats[y / b.p.len].zy;
+        o.m = zy;
+        for (int c = 0; c < b.p.parts; ++c) o.m = fmaxf(o.m, stats[c].m);
+        const Exponents ex = Exponents::of(o.m, a.log2_tau);
+        Sums sum;
+        for (int c = 0; c < b.p.parts; ++c)
+            sum.s += part_sums<false>(stats[c], o.m, ex, a.log2_tau, a.inv_tau).s;
+        const RowEnd e = row_end<false>(o.m, zy, sum, ex.off, a.inv_tau);
+        l = e.l;
+        const Slopes sl = slopes_of(e, Goal{0.0, 1.0, 0.0}, a.inv_tau);
+        o.a0 = sl.a0;
+        o.gy = sl.gy;
+    }
+    b.slope[r] = o;
+    return q.ref_logprob ? l - (double)q.ref_logprob[r] : l;
+}
+
+// the place of a row's l - ref where k_pair_rows() has formed it: its first part's sums
+__device__ __forceinline__ double* ratio_at(const PairArgs& b, int64_t r) {
+    return (double*)(b.p.stats + r * b.p.parts);
+}
+
+constexpr int kRowThreads = 256;
+
+// The rows' log-probabilities ahead of the pairs, a lane a row, for pairs of more than
+// twice the rows that their workgroup has threads for. (One pair of 16384 rows of 300
+// fp32 entries 62 -> 38 us.)
+__global__ __launch_bounds__(kRowThreads) void k_pair_rows(TokenArgs a, PreferenceArgs q, PairArgs b) {
+    const int64_t r = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
+    if (r >= a.rows) return;
+    const int y = a.tokens[r];
+    if (y != -1 && in_sequences(q, r)) *ratio_at(b, r) = row_ratio(a, q, b, r, y);
+}
+
+// A workgroup a pair: its rows' log-probabilities (or what k_pair_rows() has left of
+// them), its loss, and the slope that each of its rows takes from that.
+template <bool Formed>
 __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceArgs q, PairArgs b,
                                                        int64_t pair0) {
     constexpr int NT = kPairThreads;
@@ -548,33 +594,17 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
     }
     if (bad)
         for (int i = 0; i < 3; ++i) at[i] = min(max(at[i], (int64_t)0), a.rows);
-    const float2 c2 = a.log2_tau;
     double s[4] = {0.0, 0.0, 0.0, 0.0};   // sums of l - ref, rows, of the two sequences
+#pragma unroll Formed ? 4 : 1
     for (int64_t r = at[0] + threadIdx.x; r < at[2] && !bad; r += NT) {
         const int y = a.tokens[r];
         if (y == -1) continue;
-        double l = (double)kNan;
-        RowSlope o{0.f, kNan, kNan, 1};
-        if (y >= 0 && y < a.V) {
-            const PartStats* stats = b.p.stats + r * b.p.parts;
-            const float zy = stats[y / b.p.len].zy;
-            o.m = zy;
-            for (int c = 0; c < b.p.parts; ++c) o.m = fmaxf(o.m, stats[c].m);
-            const Exponents ex = Exponents::of(o.m, c2);
-            Sums sum;
-            for (int c = 0; c < b.p.parts; ++c) sum.s += part_sums<false>(stats[c], o.m, ex, c2, a.inv_tau).s;
-            const RowEnd e = row_end<false>(o.m, zy, sum, ex.off, a.inv_tau);
-            l = e.l;
-            const Slopes sl = slopes_of(e, Goal{0.0, 1.0, 0.0}, a.inv_tau);
-            o.a0 = sl.a0;
-            o.gy = sl.gy;
-        }
-        b.slope[r] = o;   // of l itself
-        if (q.ref_logprob) l -= (double)q.ref_logprob[r];
-        const int which = r >= at[1] ? 1 : 0;
-        s[0] += which ? 0.0 : l;
-        s[1] += which ? l : 0.0;
-        s[2 + which] += 1.0;
+        const double l = Formed ? *ratio_at(b, r) : row_ratio(a, q, b, r, y);
+        const bool rejected = r >= at[1];
+        s[0] += rejected ? 0.0 : l;
+        s[1] += rejected ? l : 0.0;
+        s[2] += rejected ? 0.0 : 1.0;
+        s[3] += rejected ? 1.0 : 0.0;
     }
     block_all<NT, 4>(s, red, AddOp());
     __shared__ double by_l[2];   // the loss's slopes by the two sequences' log-probabilities
@@ -773,8 +803,13 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
                 hipLaunchKernelGGL((k_pair_stats<T, NT, NV>), grid, dim3(NT), lds, s, a, q, b, r0);
             }, plan.parts);
     });
+    const bool formed = a.rows > 2 * kPairThreads * q.pairs;
+    if (formed)
+        hipLaunchKernelGGL(k_pair_rows, dim3((unsigned)((a.rows + kRowThreads - 1) / kRowThreads)),
+                           dim3(kRowThreads), 0, s, a, q, b);
     by_slabs(q.pairs, [&](int64_t p0, dim3 grid) {
-        hipLaunchKernelGGL(k_pair, grid, dim3(kPairThreads), 0, s, a, q, b, p0);
+        if (formed) hipLaunchKernelGGL(k_pair<true>, grid, dim3(kPairThreads), 0, s, a, q, b, p0);
+        else hipLaunchKernelGGL(k_pair<false>, grid, dim3(kPairThreads), 0, s, a, q, b, p0);
     });
     if (!a.grad) return;
     const int chunks = (a.V + kChunk2<T> - 1) / kChunk2<T>;

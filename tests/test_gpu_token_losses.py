@@ -389,6 +389,8 @@ def test_preference_of_long_sequences():
     """Sequences longer than the workgroup that adds them up."""
     preference_case(np.random.default_rng(7), [1500, 1100], 33, "f32", beta=0.01)
     preference_case(np.random.default_rng(8), [2, 2500, 1, 1], 40, "bf16", mean=True, beta=1.0)
+    preference_case(np.random.default_rng(9), [1, 2500], 40, "f16", ahead=3, behind=7, mean=True, beta=1.0)
+    preference_case(np.random.default_rng(10), [1050, 1010], 17001, "bf16", beta=0.05)
 
 
 @pytest.mark.parametrize("V", [100, 5003, 16384, 70000])
