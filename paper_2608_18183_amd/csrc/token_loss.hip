@@ -502,10 +502,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
 
 // ---- pairs of sequences
 
-// what the pair leaves for a row
+// what the pair leaves for a row: its largest logit, and what its gradient's stores need
 struct RowSlope {
     float m, a0, gy;
-    int used;
+    int used;   // 0: the row takes no part
 };
 struct PairArgs {
     PartsArgs p;
@@ -784,7 +784,7 @@ Plan pair_plan(int64_t rows, int V) {
     return p;
 }
 
-// workgroups of the second reading take 256 KB / 16 = 16 KB of a row
+// entries of a row that a workgroup of the second reading takes: 16 KB
 template <typename T> constexpr int kChunk2 = 256 * 4 * kVec<T>;
 
 template <typename T>

@@ -474,6 +474,50 @@ def test_no_rows_and_no_pairs():
     assert none.shape == (0,) and bool((g == 0).all())
 
 
+def test_gradients_equal_differences_of_what_they_belong_to():
+    """Log-probability, entropy, and the preference loss by a chosen and a rejected row."""
+    rng = np.random.default_rng(12)
+    V, tok = 260, 31
+    x = rng.normal(0, 1.5, (1, V)).astype(np.float32)
+    other = rng.normal(0, 1.5, (1, V)).astype(np.float32)
+    h = 2.0 ** -6
+    probes = np.array([tok, int(x.argmax()), 0, 1, 100, 259])
+    moved = np.repeat(x, 2 * probes.size, 0)
+    for j, v in enumerate(probes):
+        moved[2 * j, v] += np.float32(h)
+        moved[2 * j + 1, v] -= np.float32(h)
+    step = (moved[0::2, probes].diagonal().astype(np.float64)
+            - moved[1::2, probes].diagonal().astype(np.float64))
+    q = ref.Row(x[0].astype(np.float64), tok, 1.0)
+    one = dev(np.ones(1, np.float32))
+
+    def logprob(rows):
+        return P().hbsjd_logprob_rows(dev(rows), dev(np.full(len(rows), tok, np.int32)), entropy=True)
+
+    def preference(rows, which):
+        """The loss of pairs of `rows` and the other row, and the gradient by the former."""
+        z = np.repeat(other, 2 * len(rows), 0)
+        z[which::2] = rows
+        loss, grad, _ = P().hbsjd_preference_rows(dev(z), dev(np.full(len(z), tok, np.int32)), pairs=len(rows),
+                                                  beta=0.7)
+        return loss, grad[which::2]
+
+    at = dev(np.full(1, tok, np.int32))
+    cases = [(logprob(moved)[0], P().hbsjd_logprob_rows(dev(x), at, logprob_weight=one, grad=True)[2], q.l_err),
+             (logprob(moved)[1], P().hbsjd_logprob_rows(dev(x), at, entropy_weight=one, grad=True)[2],
+              q.entropy_err)]
+    both = q.l_err + ref.Row(other[0].astype(np.float64), tok, 1.0).l_err
+    for which in (0, 1):
+        cases.append((preference(moved, which)[0], preference(x, which)[1], both + 2 * U))
+    for value, grad, err in cases:
+        f = value.double().cpu().numpy()
+        d = (f[0::2] - f[1::2]) / step
+        got = grad[0].double().cpu().numpy()[probes]
+        # two values' errors over the step, and h^2 / 6 times a third derivative: l's is at
+        # most 1, H's and the loss's below 8 for these rows
+        assert np.abs(d - got).max() <= 2 * err / (2 * h) * 1.1 + h * h / 6 * 8
+
+
 # ------------------------------------------------------------------ as calls
 
 def all_three(x, tok, f, stream=None):
@@ -579,7 +623,7 @@ def test_same_bits_alone_or_among_rows():
 
 
 @pytest.mark.parametrize("rows,V,dtype", [(6144, 16384, "f32"), (4608, 16384, "bf16"), (300, 60000, "f16"),
-                                          (300, 80001, "f16"), (420, 50001, "f32"),
+                                          (300, 80001, "f16"), (420, 50001, "f32"), (4200, 16381, "bf16"),
                                           (130, 128257, "bf16"), (70000, 40, "f32"), (2_200_000, 3, "f16")])
 def test_batches(rows, V, dtype):
     """Batches of whole images, long and short rows, more rows than a launch takes:
@@ -593,6 +637,13 @@ def test_batches(rows, V, dtype):
     d, dg, s = P().hbsjd_preference_rows(x, tok, pairs=rows // 2, ref_logprob=f, beta=0.5)
     for o in (*out, loss, pg, d, dg, s):
         assert bool(torch.isfinite(o).all())
+    y = x.clone()
+    P().hbsjd_policy_rows(y, tok, f, entropy_weight=0.1, grad=y)
+    assert torch.equal(y, pg)
+    y.copy_(x)
+    P().hbsjd_preference_rows(y, tok, pairs=rows // 2, ref_logprob=f, beta=0.5, grad=y)
+    assert torch.equal(y, dg)
+    del y
     rng = np.random.default_rng(0)
     pick = np.unique(np.concatenate([[0, 1, rows - 2, rows - 1], rng.integers(0, rows, 4)]))
     at = torch.from_numpy(pick).cuda()
