@@ -8,12 +8,13 @@
 // of the scaling adds them up for itself in the same order, which saves a launch.
 //
 // Memory alone bounds both passes (squares in 64 bits or 32: 45.9 and 45.4 us for the
-// 222 MB of the B model). What the second pass finds of the first one's reading in the
-// last-level cache (256 MB) is not read again: the tensors' last kKeep bytes are read as
-// usual, those before them and all of the second pass as streams, and the second pass
-// starts from the end. Clipping 111 M bf16 entries (222 MB) into others, both passes'
-// kernels: all loads and stores as usual 120 us, stores alone as streams 104, and the
-// second pass's loads 105; 757 M fp32 ones 1706, 1664, 1582.
+// 222 MB of the B model). The norm's pass reads the tensors' last kKeep bytes, which the
+// second pass may find in the last-level cache (256 MB), as usual, and those before them
+// as streams; in long lists the second pass is streams throughout. Clipping 111 M bf16
+// entries (222 MB) into others, both passes' kernels: all loads and stores as usual 120
+// us, stores alone as streams 104, the second pass's loads too 105, the norm's too 119;
+// 757 M fp32 ones 1706, 1664, 1582, 1561, and 1535 with the norm's but for the last
+// kKeep. (The second pass from the end on: the same.)
 #include "grad_norm.h"
 
 #include <algorithm>
@@ -218,8 +219,6 @@ __device__ __forceinline__ void scale_unit(const Tab& t, int i, uint32_t u, floa
     }
 }
 
-// A workgroup's units, the last one first: the norm's pass has left those in the
-// last-level cache.
 template <typename A, typename Tab>
 __global__ __launch_bounds__(NT) void k_scale(Tab t, const A* part, int groups, float limit, float* norm) {
     __shared__ A red[NT / 64];
@@ -228,11 +227,10 @@ __global__ __launch_bounds__(NT) void k_scale(Tab t, const A* part, int groups, 
     const bool scaled = n > (double)limit && n < INFINITY;
     if (!Tab::kOut && !scaled) return;
     const float f = uniform(scaled ? (float)((double)limit / n) : 1.f);
-    const uint32_t mine = (t.unit[t.count] - 1 - blockIdx.x) / t.groups;   // the last of this workgroup's
-    uint32_t u = blockIdx.x + mine * t.groups;
-    int i = tensor_of(t, u);
-    for (uint32_t left = mine + 1; left > 0; --left, u -= t.groups) {
-        while (u < t.unit[i]) --i;
+    uint32_t u = blockIdx.x;
+    const uint32_t end = t.unit[t.count];
+    for (int i = tensor_of(t, u); u < end; u += t.groups) {
+        while (u >= t.unit[i + 1]) ++i;
         const uint32_t k = u - t.unit[i];
         auto with = [&](auto type) {
             using T = decltype(type);
@@ -255,19 +253,16 @@ uint32_t units_of(const void* p, int64_t n, int32_t elem) {
     return (uint32_t)std::max<int64_t>(1, (s.vecs + kUnit - 1) / kUnit);
 }
 
-// f(table) for the tensors, in launches of equal numbers of them, from the first on or
-// from the last
-template <typename Tab, typename F> void by_tables(const GradArgs& a, bool from_last, F f) {
+// f(table) for the tensors in order, in launches of equal numbers of them
+template <typename Tab, typename F> void by_tables(const GradArgs& a, F f) {
     const int64_t launches = (a.count + Tab::kTensors - 1) / Tab::kTensors;
     if (launches == 0) return;
     const int64_t each = (a.count + launches - 1) / launches;
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kGroups, kPartials / launches));
     Tab t;
     t.first_group = 0;
-    for (int64_t l = 0; l < launches; ++l) {
-        const int64_t i0 = (from_last ? launches - 1 - l : l) * each;
+    for (int64_t i0 = 0; i0 < a.count; i0 += each) {
         t.count = (int)std::min<int64_t>(each, a.count - i0);
-        if (t.count <= 0) continue;
         uint32_t units = 0;
         for (int i = 0; i < t.count; ++i) {
             t.in[i] = a.data[i0 + i];
@@ -287,7 +282,7 @@ template <typename Tab, typename F> void by_tables(const GradArgs& a, bool from_
 template <typename A, typename Tab>
 void scale(const GradArgs& a, const A* part, int groups, bool stream, hipStream_t s) {
     float* norm = a.norm;
-    by_tables<Tab>(a, true, [&](Tab& t) {
+    by_tables<Tab>(a, [&](Tab& t) {
         t.stream = stream ? UINT32_MAX : 0;
         hipLaunchKernelGGL((k_scale<A, Tab>), dim3(t.groups), dim3(NT), 0, s, t, part, groups, a.limit, norm);
         norm = nullptr;   // the first launch writes it
@@ -301,7 +296,7 @@ template <typename A> bool go(const GradArgs& a, void* ws, hipStream_t s) {
     if (units > UINT32_MAX) return false;
     int groups = 0;
     uint64_t done = 0;
-    by_tables<Inputs>(a, false, [&](Inputs& t) {
+    by_tables<Inputs>(a, [&](Inputs& t) {
         // the call's units from here on that are not among its last kKeep
         const uint64_t mine = t.unit[t.count];
         const uint64_t streams = units > done + kKeep ? units - done - kKeep : 0;

@@ -456,7 +456,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
     const int64_t r = r0 + row;
     const int y = a.tokens[r];
     if (y < 0 || y >= a.V || (a.weight && a.weight[r] == 0.f)) return;
-    part_stats<T, NT, NV, Ent>(a, p, r, c, y, p.stats + (int64_t)row * p.parts + c, false);
+    part_stats<T, NT, NV, Ent>(a, p, r, c, y, p.stats + (int64_t)row * p.parts + c, a.stream && !a.grad);
 }
 
 // Joins a row's parts (every part's workgroup does, a lane a part) and stores the
@@ -660,12 +660,13 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
     }
 }
 
-// The second reading: the gradient. The last rows come first: the first reading
-// has left them in the last-level cache.
+// The second reading: the gradient. (From the last rows on, those that the first reading
+// has left in the last-level cache, it is slower: 32 pairs of 256 fp32 rows of 16384 526
+// us, so 515.)
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_pair_grad(TokenArgs a, PairArgs b, int chunks, int len, int64_t r1) {
+__global__ __launch_bounds__(NT) void k_pair_grad(TokenArgs a, PairArgs b, int chunks, int len, int64_t r0) {
     const int row = blockIdx.x / chunks, c = blockIdx.x - row * chunks;
-    const int64_t r = r1 - 1 - row;
+    const int64_t r = r0 + row;
     const int first = c * len, V = min(len, a.V - first);
     const T* z = (const T*)a.logits + r * a.ld + first;
     T* g = (T*)a.grad + r * a.ld_grad + first;
@@ -763,7 +764,9 @@ template <typename T, bool Ent> void go(const TokenArgs& a, void* ws, hipStream_
 // probabilities of 6144 fp32 rows of 16384 72, 72, 65 us; policy loss and gradient there
 // 147, 141, 142; gradients of 18432 bf16 rows 195, 191, 177; 8192 bf16 rows in pairs 132,
 // 121, 120; 4 pairs of 101 bf16 rows of 128257 104, 97, 89. (Of less, what reads the
-// gradient next finds it in the cache.)
+// gradient next finds it in the cache.) The first reading of pairs is streams but for its
+// last 192 MB, which the second one may find in the last-level cache of 256 (the 8192
+// rows 119 us without, 116).
 constexpr int64_t kSmall = 64 << 20, kCached = 192 << 20;
 template <typename T> TokenArgs streamed(const TokenArgs& a) {
     TokenArgs b = a;
@@ -793,7 +796,7 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
     const Plan plan = pair_plan(a.rows, a.V);
     PairArgs b;
     b.slope = (RowSlope*)ws;
-    b.streams = std::max<int64_t>(0, a.rows - kCached / (int64_t)(a.V * sizeof(T)));
+    b.streams = a.rows - kCached / (int64_t)(a.V * sizeof(T));
     b.p = PartsArgs{plan.parts, plan.len, (PartStats*)(b.slope + a.rows)};
     const size_t lds = resident_lds(0, plan.len * sizeof(T));
     by_size<T>(plan.len, [&](auto nt, auto nv) {
@@ -817,11 +820,9 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
     by_size<T>(len, [&](auto nt, auto nv) {
         constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
         if constexpr (NT * NV <= 1024) {   // up to kChunk2
-            const int64_t slab = (1 << 21) / chunks;
-            for (int64_t r1 = a.rows; r1 > 0; r1 -= slab) {
-                const dim3 grid((unsigned)(std::min(slab, r1) * chunks));
-                hipLaunchKernelGGL((k_pair_grad<T, NT, NV>), grid, dim3(NT), 0, s, a, b, chunks, len, r1);
-            }
+            by_slabs(a.rows, [&](int64_t r0, dim3 grid) {
+                hipLaunchKernelGGL((k_pair_grad<T, NT, NV>), grid, dim3(NT), 0, s, a, b, chunks, len, r0);
+            }, chunks);
         }
     });
 }
