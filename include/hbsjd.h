@@ -569,8 +569,8 @@ hbsjd_status hbsjd_grad_norm(int64_t count, const void* const* data, const int64
                              uint64_t workspace_bytes, void* stream);
 
 /*
- * As above, and out[i] = data[i] * limit / norm where the norm is above the limit
- * (the quotient rounded once to fp32, each product once to the tensor's type), else
+ * As above, and out[i] = data[i] * (limit / norm) where the norm is above the limit (the
+ * quotient and the products in fp32, rounded once more to 16-bit tensors' types), else
  * out[i] = data[i]. `out` NULL: the tensors themselves, which are then not written
  * unless they are scaled. A norm that is not finite (before it is rounded to fp32)
  * scales nothing. out[i] is of data[i]'s type and size; written tensors overlap
