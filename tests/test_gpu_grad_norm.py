@@ -179,6 +179,21 @@ def test_squares_past_fp32():
     assert torch.equal(x, keep)
 
 
+def test_subnormal_entries():
+    """The smallest numbers of each type count, and are scaled as others are."""
+    for dtype, tiny in (("f32", 3e-40), ("bf16", 3e-39), ("f16", 1.3e-7)):
+        x = torch.full((5003,), tiny, device="cuda").to(TYPES[dtype])
+        want = norm64([x], 2)
+        assert want > 0
+        # where the norm is subnormal itself it is rounded to a multiple of 2^-149
+        assert abs(float(P().hbsjd_grad_norm([x])) - want) <= 1.001 * U * want + 2.0 ** -150
+        assert float(P().hbsjd_grad_norm([x], order=math.inf)) == float(x[0])
+        before = x.clone()
+        limit = float(np.float32(want / 4))
+        P().hbsjd_clip_grads([x], limit)
+        check_scaled(x, before, limit / want)
+
+
 def test_more_entries_than_32_bits_count():
     """One bf16 tensor of 2^32 + 77 entries: its last ones count and are scaled."""
     n = 2 ** 32 + 77
