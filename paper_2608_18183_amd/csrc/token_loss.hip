@@ -592,6 +592,8 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
         at[i] = q.first ? (int64_t)q.first[s] : s * (a.rows / (2 * q.pairs));
         if (at[i] < 0 || at[i] > a.rows || (i && at[i] < at[i - 1])) bad = true;
     }
+    // rows that in_sequences() leaves out have no sums
+    if (q.first && (at[0] < q.first[0] || at[2] > q.first[2 * q.pairs])) bad = true;
     if (bad)
         for (int i = 0; i < 3; ++i) at[i] = min(max(at[i], (int64_t)0), a.rows);
     double s[4] = {0.0, 0.0, 0.0, 0.0};   // sums of l - ref, rows, of the two sequences

@@ -1,0 +1,57 @@
+"""Preference losses of packed pairs whose offsets are not all in order: which pairs are in
+error, and what their rows' gradients hold."""
+import numpy as np
+import pytest
+
+from tests import test_gpu_row_operators as ops
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+P, dev = ops.P, ops.dev
+
+# A short batch, and one so long that the rows are worked out ahead of the pairs.
+SCALES = [1, 400]
+
+
+def batch(scale, V=50):
+    rng = np.random.default_rng(scale)
+    rows = 12 * scale
+    x = rng.normal(0, 1, (rows, V)).astype(np.float32)
+    tok = rng.integers(0, V, rows).astype(np.int32)
+    return dev(x), dev(tok)
+
+
+def call(x, tok, first, scale, **kw):
+    return P().hbsjd_preference_rows(x, tok, first=dev(np.array(first, np.int32) * scale), **kw)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+def test_pairs_outside_the_outermost_offsets(scale):
+    """A pair that reaches ahead of the first offset or behind the last one is in error,
+    though its own offsets ascend; the rows there are nobody's and have no sums."""
+    x, tok = batch(scale)
+    sound = call(x, tok, [0, 2, 4, 7, 12], scale)
+    for first, outside in (([5, 2, 4, 7, 12], 1), ([0, 2, 4, 7, -1], 0), ([0, 6, 12, 8, 10], 0),
+                           ([3, 2, 4, 7, 12], 0), ([3, 3, 3, 2, 2], 0)):
+        # the workspace that the call gets holds what another one has left there
+        call(x, tok, [0, 2, 4, 7, 12], scale)
+        loss, grad, s = call(x, tok, first, scale)
+        at = [v * scale for v in first[2 * outside:2 * outside + 3]]
+        assert bool(torch.isnan(loss[outside])), first
+        assert bool(torch.isnan(s[2 * outside:2 * outside + 2]).all()), first
+        if at[0] <= at[1] <= at[2]:
+            assert bool(torch.isnan(grad[at[0]:at[2]]).all()), first
+    again = call(x, tok, [0, 2, 4, 7, 12], scale)
+    assert all(torch.equal(a, b) for a, b in zip(again, sound))
+
+
+@pytest.mark.parametrize("scale", SCALES)
+def test_rows_outside_the_outermost_offsets_are_left_out(scale):
+    """With offsets in order the same rows as without the others."""
+    x, tok = batch(scale)
+    loss, grad, s = call(x, tok, [2, 3, 5, 7, 9], scale)
+    part = slice(2 * scale, 9 * scale)
+    want = call(x[part], tok[part], [0, 1, 3, 5, 7], scale)
+    assert torch.equal(loss, want[0]) and torch.equal(s, want[2]) and torch.equal(grad[part], want[1])
+    assert bool((grad[:2 * scale] == 0).all()) and bool((grad[9 * scale:] == 0).all())
