@@ -545,8 +545,9 @@ typedef struct hbsjd_preference_args {
  * log_ratio). A row in error makes its pair's loss NaN. A pair is in error too (its
  * loss and log ratios are NaN) where its entries of `first` descend, leave [0, rows]
  * or lie outside first[0] to first[2 pairs]. A pair whose loss is not finite has NaN in the
- * gradient of its rows that have a token (where pairs in error claim others' rows,
- * either's). EINVAL; EHIP.
+ * gradient of its rows that have a token, and so has a row with a token that two pairs
+ * hold (offsets that descend allow that; the losses of pairs in order stay). EINVAL;
+ * EHIP.
  */
 hbsjd_status hbsjd_preference_rows(const hbsjd_preference_args* args, float* loss, float* log_ratio,
                                    void* grad, int64_t ld_grad, void* workspace,

@@ -502,14 +502,16 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(waves_of(NT)
 
 // ---- pairs of sequences
 
-// what the pair leaves for a row: its largest logit, and what its gradient's stores need
+// A row's largest logit, what the stores of its log-probability's gradient need, and
+// how many pairs take it as one of theirs (two do where offsets descend).
 struct RowSlope {
     float m, a0, gy;
-    int used;   // 0: the row takes no part
+    int pairs;
 };
 struct PairArgs {
     PartsArgs p;
     RowSlope* slope;   // [rows]
+    float2* scaled;    // [rows], a0 and gy times what the row's pair makes of them
     int64_t streams;   // rows that the second reading will not find in the caches
 };
 
@@ -539,7 +541,7 @@ __device__ __forceinline__ double logistic(double x) { return 1.0 / (1.0 + exp(-
 // l - ref of a row that has a token, from its parts; leaves the slopes of l
 __device__ __forceinline__ double row_ratio(const TokenArgs& a, const PreferenceArgs& q, const PairArgs& b,
                                             int64_t r, int y) {
-    RowSlope o{0.f, kNan, kNan, 1};
+    RowSlope o{0.f, kNan, kNan, 0};
     double l = (double)kNan;
     if (y >= 0 && y < a.V) {
         const PartStats* stats = b.p.stats + r * b.p.parts;
@@ -556,7 +558,10 @@ __device__ __forceinline__ double row_ratio(const TokenArgs& a, const Preference
         o.a0 = sl.a0;
         o.gy = sl.gy;
     }
-    b.slope[r] = o;
+    RowSlope& slope = b.slope[r];   // (another pair may count itself there meanwhile)
+    slope.m = o.m;
+    slope.a0 = o.a0;
+    slope.gy = o.gy;
     return q.ref_logprob ? l - (double)q.ref_logprob[r] : l;
 }
 
@@ -651,14 +656,14 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
     __syncthreads();
     for (int64_t r = at[0] + threadIdx.x; r < (bad ? max(at[1], at[2]) : at[2]); r += NT) {
         if (a.tokens[r] == -1) continue;
-        RowSlope o{0.f, kNan, kNan, 1};
+        float2 y = make_float2(kNan, kNan);
         if (sound) {
-            o = b.slope[r];
             const double f = by_l[r >= at[1] ? 1 : 0];
-            o.a0 = f == 0.0 ? 0.f : (float)(o.a0 * f);   // (a row in error weighted out)
-            o.gy = f == 0.0 ? 0.f : (float)(o.gy * f);
+            y.x = f == 0.0 ? 0.f : (float)(b.slope[r].a0 * f);   // (a row in error weighted out)
+            y.y = f == 0.0 ? 0.f : (float)(b.slope[r].gy * f);
         }
-        b.slope[r] = o;
+        b.scaled[r] = y;   // of no use where another pair stores its own
+        atomicAdd(&b.slope[r].pairs, 1);
     }
 }
 
@@ -673,9 +678,11 @@ __global__ __launch_bounds__(NT) void k_pair_grad(TokenArgs a, PairArgs b, int c
     const T* z = (const T*)a.logits + r * a.ld + first;
     T* g = (T*)a.grad + r * a.ld_grad + first;
     const RowSlope o = b.slope[r];
-    const float a0 = uniform(o.a0), gy = uniform(o.gy), m = uniform(o.m);
-    if (!uniform(o.used) || (a0 == 0.f && gy == 0.f)) return fill_row<NT>(g, V, 0.f);
-    if (a0 != a0 || gy != gy) return fill_row<NT>(g, V, kNan);
+    const float2 y = b.scaled[r];   // none where no pair has the row
+    const float a0 = uniform(y.x), gy = uniform(y.y), m = uniform(o.m);
+    const int pairs = uniform(o.pairs);
+    if (pairs == 0 || (pairs == 1 && a0 == 0.f && gy == 0.f)) return fill_row<NT>(g, V, 0.f);
+    if (pairs > 1 || a0 != a0 || gy != gy) return fill_row<NT>(g, V, kNan);
     TokenRow<T, NT, NV> part;
     part.load(z, V, a.stream);
     part.find(a.tokens[r] - first, V);
@@ -800,6 +807,7 @@ void go_pairs(const TokenArgs& args, const PreferenceArgs& q, void* ws, hipStrea
     b.slope = (RowSlope*)ws;
     b.streams = a.rows - kCached / (int64_t)(a.V * sizeof(T));
     b.p = PartsArgs{plan.parts, plan.len, (PartStats*)(b.slope + a.rows)};
+    b.scaled = (float2*)(b.p.stats + a.rows * plan.parts);
     const size_t lds = resident_lds(0, plan.len * sizeof(T));
     by_size<T>(plan.len, [&](auto nt, auto nv) {
         constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
@@ -844,7 +852,7 @@ void token_rows(const TokenArgs& a, void* workspace, hipStream_t s) {
 
 size_t preference_workspace(int64_t rows, int V, int32_t) {
     const Plan p = pair_plan(rows, V);
-    return (size_t)rows * (sizeof(RowSlope) + p.parts * sizeof(PartStats));
+    return (size_t)rows * (sizeof(RowSlope) + p.parts * sizeof(PartStats) + sizeof(float2));
 }
 
 void preference_rows(const TokenArgs& a, const PreferenceArgs& p, void* workspace, hipStream_t s) {

@@ -55,3 +55,24 @@ def test_rows_outside_the_outermost_offsets_are_left_out(scale):
     want = call(x[part], tok[part], [0, 1, 3, 5, 7], scale)
     assert torch.equal(loss, want[0]) and torch.equal(s, want[2]) and torch.equal(grad[part], want[1])
     assert bool((grad[:2 * scale] == 0).all()) and bool((grad[9 * scale:] == 0).all())
+
+
+@pytest.mark.parametrize("scale", SCALES)
+def test_rows_that_two_pairs_hold(scale):
+    """Pairs 0 and 2 are in order and share the rows 4 and 5: losses as of any pair, NaN in
+    the shared rows' gradient, each pair's own in the others, the same at every call."""
+    x, tok = batch(scale)
+    tok[4 * scale] = -1
+    first = [0, 3, 6, 2, 4, 5, 9]
+    loss, grad, s = call(x, tok, first, scale, beta=0.7)
+    assert bool(torch.isnan(loss[1])) and bool(torch.isnan(s[2:4]).all())
+    for pair, own in ((0, slice(0, 2 * scale)), (2, slice(6 * scale, 9 * scale))):
+        lone = call(x, tok, first[2 * pair:2 * pair + 3], scale, beta=0.7)
+        assert torch.equal(loss[pair], lone[0][0]) and torch.equal(s[2 * pair:2 * pair + 2], lone[2])
+        assert torch.equal(grad[own], lone[1][own])
+    assert bool((grad[4 * scale] == 0).all())       # no token
+    assert bool(torch.isnan(grad[4 * scale + 1:6 * scale]).all())
+    assert bool((grad[9 * scale:] == 0).all())
+    for _ in range(5):
+        again = call(x, tok, first, scale, beta=0.7)
+        assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(again, (loss, grad, s)))
