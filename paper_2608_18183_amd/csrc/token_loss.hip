@@ -654,7 +654,8 @@ __global__ __launch_bounds__(kPairThreads) void k_pair(TokenArgs a, PreferenceAr
     }
     if (!a.grad) return;
     __syncthreads();
-    for (int64_t r = at[0] + threadIdx.x; r < (bad ? max(at[1], at[2]) : at[2]); r += NT) {
+    // a pair in error may have one sequence that descends: the other one's rows are its
+    for (int64_t r = min(at[0], at[1]) + threadIdx.x; r < max(at[1], at[2]); r += NT) {
         if (a.tokens[r] == -1) continue;
         float2 y = make_float2(kNan, kNan);
         if (sound) {

@@ -76,3 +76,21 @@ def test_rows_that_two_pairs_hold(scale):
     for _ in range(5):
         again = call(x, tok, first, scale, beta=0.7)
         assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(again, (loss, grad, s)))
+
+
+@pytest.mark.parametrize("scale", SCALES)
+def test_rows_of_pairs_in_error(scale):
+    """Their two sequences' rows have NaN, one that descends has no rows; a row that is
+    another pair's too is shared; the rest is left out or the other pair's."""
+    x, tok = batch(scale)
+    tok[7 * scale] = -1
+    for first, none in (([0, 2, 4, 3, 12], [(3, 12)]), ([5, 2, 4, 7, 12], [(2, 12)]), ([0, 4, 2, 7, 12], [(0, 4)]),
+                        ([0, 2, 9, 4, 12], [(4, 12)]), ([0, 2, 4, 7, 13], [(4, 12)]), ([-5, 2, 4, 7, 12], [(0, 4)]),
+                        ([12, 11, 10, 9, 8], []), ([6, 4, 5, 3, 2], [(4, 5)]), ([1, 5, 3, 3, 3], [(1, 5)])):
+        want = torch.zeros(12 * scale, dtype=torch.bool, device="cuda")
+        for a, b in none:
+            want[a * scale:b * scale] = True
+        want[7 * scale] = False                      # no token
+        _, grad, _ = call(x, tok, first, scale)
+        assert torch.equal(torch.isnan(grad).all(1), want), first
+        assert torch.equal(torch.isnan(grad).any(1), want), first
