@@ -540,14 +540,14 @@ typedef struct hbsjd_preference_args {
 
 /*
  * loss: fp32 [pairs] or NULL; log_ratio: s of every sequence, fp32 [2 pairs] or NULL;
- * not all three outputs NULL. Rows are read twice where there is a gradient. A pair
- * with w_i = 0 has the loss 0 and no gradient (its rows are read once, for
- * log_ratio). A row in error makes its pair's loss NaN. A pair is in error too (its
- * loss and log ratios are NaN) where its entries of `first` descend, leave [0, rows]
- * or lie outside first[0] to first[2 pairs]. A pair whose loss is not finite has NaN in the
- * gradient of its rows that have a token, and so has a row with a token that two pairs
- * hold (offsets that descend allow that; the losses of pairs in order stay). EINVAL;
- * EHIP.
+ * not all three outputs NULL where there are pairs. Rows are read twice where there is
+ * a gradient. A pair with w_i = 0 has the loss 0 and no gradient (its rows are read
+ * once, for log_ratio). A row in error makes its pair's loss NaN. A pair is in error
+ * too (its loss and log ratios are NaN) where its entries of `first` descend, leave
+ * [0, rows] or lie outside first[0] to first[2 pairs]. A pair whose loss is not finite
+ * has NaN in the gradient of its rows that have a token, and so has a row with a token
+ * that two pairs hold (offsets that descend allow that; the losses of pairs in order
+ * stay). EINVAL; EHIP.
  */
 hbsjd_status hbsjd_preference_rows(const hbsjd_preference_args* args, float* loss, float* log_ratio,
                                    void* grad, int64_t ld_grad, void* workspace,

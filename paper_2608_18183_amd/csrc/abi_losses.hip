@@ -208,7 +208,8 @@ hbsjd_status hbsjd_preference_rows(const hbsjd_preference_args* p, float* loss, 
         if (!p->first && (p->pairs ? p->rows % (2 * p->pairs) : p->rows))
             return api_fail(HBSJD_EINVAL, "without first the rows have to be a multiple of 2 pairs");
         if (p->rows == 0 && p->pairs == 0) return HBSJD_OK;
-        if (!loss && !log_ratio && !grad) return api_fail(HBSJD_EINVAL, "no output");
+        // (without pairs the outputs have no entries, and an empty tensor no address)
+        if (p->pairs && !loss && !log_ratio && !grad) return api_fail(HBSJD_EINVAL, "no output");
         if (p->rows)
             if (const char* why = token_problem(p, grad, ld_grad)) return api_fail(HBSJD_EINVAL, why);
         if (!all_aligned({loss, log_ratio, p->first, p->ref_logprob, p->pair_weight}))
@@ -216,6 +217,7 @@ hbsjd_status hbsjd_preference_rows(const hbsjd_preference_args* p, float* loss, 
         const uint64_t need = p->rows ? preference_workspace(p->rows, p->V, p->elem) : 0;
         if (const char* why = workspace_problem(workspace, workspace_bytes, need))
             return api_fail(HBSJD_EINVAL, why);
+        if (p->pairs == 0 && !grad) return HBSJD_OK;
         const TokenArgs a = token_args(p, grad, ld_grad);
         const PreferenceArgs q{p->pairs, p->first, p->ref_logprob, p->form, p->mean != 0, p->beta, p->smoothing,
                                p->margin, p->pair_weight, loss, log_ratio};
