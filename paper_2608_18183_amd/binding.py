@@ -895,6 +895,7 @@ def _described(tensors, what: str, device):
     whether all are contiguous. (Lists may be hundreds long: one pass in C for each
     property takes 25 ns a tensor, the loop below ten times that.)"""
     T, types = _torch.Tensor, _ELEMS
+    kinds = None
     try:
         at = array.array("Q", list(map(T.data_ptr, tensors)))
         sizes = array.array("q", list(map(T.numel, tensors)))
@@ -912,6 +913,8 @@ def _described(tensors, what: str, device):
                 raise ValueError(f"{what}: fp32, bf16 or fp16, not {t.dtype}")
             if not _dense(t):
                 raise ValueError(f"{what}: a tensor's entries have to lie one after another")
+        if kinds is None:   # a function transform's, for instance
+            raise ValueError(f"{what}: expected tensors with an address")
     if len(kinds) == 1:
         return at, sizes, array.array("i", [types[dtypes[0]]]) * len(dtypes), flat
     return at, sizes, array.array("i", [types[t] for t in dtypes]), flat
