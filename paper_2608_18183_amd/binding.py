@@ -887,6 +887,13 @@ def _dense(t) -> bool:
     return True
 
 
+def _alike(a, b) -> bool:
+    """Whether the entries of two dense tensors of one size lie in the same order."""
+    if a.is_contiguous() and b.is_contiguous():
+        return a.numel() == b.numel()
+    return a.shape == b.shape and all(s == t for n, s, t in zip(a.shape, a.stride(), b.stride()) if n != 1)
+
+
 _dtype_of = operator.attrgetter("dtype")
 
 
@@ -980,7 +987,7 @@ def hbsjd_clip_grads(grads, limit: float, order: float = 2.0, out=None, stream=N
         out_at, out_sizes, out_elems, out_flat = _described(out, "out", dev)
         alike = out_sizes == sizes and out_elems == elems
         if alike and not (flat and out_flat):
-            alike = all(g.shape == o.shape and g.stride() == o.stride() for g, o in zip(grads, out))
+            alike = all(map(_alike, grads, out))
         if not alike:
             raise ValueError("out: expected tensors of the same sizes, types and strides")
     norm = torch.empty((), dtype=torch.float32, device=dev)
