@@ -174,6 +174,13 @@ __device__ __forceinline__ void listed_gradient(const DistillArgs& a, const Entr
     }
 }
 
+// exp(d / tau): log2 e / tau in two parts, since the rounding of one alone would
+// put all entries of the sum off the same way. (Both are positive: d = -infinity
+// gives 0.)
+__device__ __forceinline__ float power(float d, float2 c2) {
+    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
+}
+
 // ---- a row, or a part of one, in registers: NV 16-byte vectors a thread
 
 template <typename T, int NT, int NV> struct Held : RowRegs<T, NT, NV> {

@@ -209,13 +209,6 @@ __device__ __forceinline__ float exp_of(double x) {
     return h < -200.f ? 0.f : fmaf(e, (float)(u - (double)h) * kLn2, e);
 }
 
-// exp(d / tau): log2 e / tau in two parts, since the rounding of one alone would
-// put all entries of the sum off the same way. (Both are positive: d = -infinity
-// gives 0.)
-__device__ __forceinline__ float power(float d, float2 c2) {
-    return __builtin_amdgcn_exp2f(fmaf(d, c2.x, d * c2.y));
-}
-
 // ------------------------------------------------------------ rows in registers
 // a row of one value
 template <int NT, typename T>
@@ -347,7 +340,7 @@ struct TokenArgs {
     int64_t ld;
     const int32_t* tokens;         // [rows], -1: the row takes no part
     double inv_tau;
-    float2 log2_tau;               // log2 e / temperature in two parts
+    float2 log2_tau;               // log2 e / temperature in two parts (used as their sum)
     void* grad;                    // [rows], stride ld_grad, or null
     int64_t ld_grad;
     bool stream;                   // rows and gradients are past what the caches hold
