@@ -2,11 +2,12 @@
 fp32 exponentials and sums may differ from them by.
 
 Bounds, with U half a step of fp32 and y_v = (largest logit - z_v) / tau >= 0:
-* an exponential's argument takes two roundings (difference, fused product; the
-  factor log2 e / tau is held in two parts), the hardware's exp2 is good to a step: a
-  term's relative error is U (2 y_v + 2). Where a gradient is stored in 16 bits the
-  factor is one number, which adds a step of the argument: U (4 y_v + 2).
-* a sum is a tree over a vector's 8 entries at most, a chain over 16 vectors at most
+* an exponential's argument takes two roundings (the factor log2 e / tau, which is one
+  fp32 number, and the fused operation), the hardware's exp2 is good to a step: a
+  term's relative error is U (2 y_v + 2). The bound of a gradient stored in 16 bits
+  counts U (4 y_v + 2), more than the steps take (tests/test_gpu_token_losses_bounds.py
+  holds such gradients to 2 y_v + 2).
+* a sum is a chain over a vector's 8 entries at most, a chain over 16 vectors at most
   and an edge entry in fp32 (26 roundings at most), then in 64 bits; a row in parts
   adds one rounding of a part's sum and one exponential of its offset (2 roundings'
   worth of argument that y_v counts, 2 U). The weighted mean of y_v is below ln n.
