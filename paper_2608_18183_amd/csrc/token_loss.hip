@@ -62,8 +62,8 @@ struct Sums {
     double s = 0.0, t = 0.0;   // sums of e and e x, without the token's entry
 };
 
-// the largest entry of a vector, and m; a NaN counts for nothing, and a bf16 infinity
-// may not either (the sum is none then)
+// the largest entry of a vector, and m; a NaN counts for nothing, or for all there was
+// (the sum is none then)
 template <typename T> struct Largest {
     float m = -INFINITY;
     __device__ __forceinline__ void add(const u32x4& v) {
@@ -72,20 +72,20 @@ template <typename T> struct Largest {
     }
     __device__ __forceinline__ float get() const { return m; }
 };
-// as pairs: an upper entry as the float that its pair is, whose other digits change no
-// order between different ones
+// as pairs. The upper entry without the lower one's digits, which would make a masked
+// entry's -infinity a signalling NaN: the hardware's maximum of that and all before it is a
+// NaN, and the next one leaves it out. (The integers' packed maximum and minimum, two
+// operations a pair for four, take 5% more in readings of long rows.)
 template <> struct Largest<Bf16> {
     float lo = -INFINITY, hi = -INFINITY;
     __device__ __forceinline__ void add(const u32x4& v) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             lo = fmaxf(lo, __uint_as_float(v[q] << 16));
-            hi = fmaxf(hi, __uint_as_float(v[q]));
+            hi = fmaxf(hi, __uint_as_float(v[q] & 0xFFFF0000u));
         }
     }
-    __device__ __forceinline__ float get() const {
-        return fmaxf(lo, __uint_as_float(__float_as_uint(hi) & 0xFFFF0000u));
-    }
+    __device__ __forceinline__ float get() const { return fmaxf(lo, hi); }
 };
 template <> struct Largest<F16> {
     f16x2 m = {(_Float16)-INFINITY, (_Float16)-INFINITY};
