@@ -244,7 +244,7 @@ constexpr double kLn2d = 0.6931471805599453094;
 struct RowEnd {
     double l, entropy;
     double s, se, ey;   // sums of e: the row's, without the token, the token's
-    double xy, mean;    // the token's exponent and the mean of all, in nats
+    double mean, over;  // the mean of all exponents in nats, and what the token's is above it
 };
 
 // a condition; One: every lane of the wavefront has the same
@@ -259,8 +259,8 @@ template <bool One>
 __device__ __forceinline__ RowEnd row_end(float m, float zy, Sums o, double off, double inv_tau) {
     RowEnd r;
     const double x = ((double)zy - (double)m) * inv_tau;
-    r.xy = x + off;
-    r.ey = exp_of(r.xy);
+    const double xy = x + off;
+    r.ey = exp_of(xy);
     r.se = o.s;
     r.s = o.s + r.ey;
     // a token that has most of the mass is the largest entry: x is 0
@@ -268,9 +268,12 @@ __device__ __forceinline__ RowEnd row_end(float m, float zy, Sums o, double off,
     double up;
     if (most) up = log1p(o.s / r.ey);
     else up = log(r.s);
-    r.l = most ? -up : r.xy - up;
-    r.mean = (o.t * kLn2d + (r.ey > 0.0 ? r.ey * r.xy : 0.0)) / r.s;
-    r.entropy = (most ? up + r.xy : up) - r.mean;
+    r.l = most ? -up : xy - up;
+    const double per = 1.0 / r.s;
+    r.mean = (o.t * kLn2d + (r.ey > 0.0 ? r.ey * xy : 0.0)) * per;
+    // xy - mean, which for a token that is nearly certain are almost equal
+    r.over = r.ey > 0.0 ? (xy * o.s - o.t * kLn2d) * per : 0.0;
+    r.entropy = most ? up + r.over : up - r.mean;
     // no distribution: nothing left, a NaN or an infinity (the sums are then 0 or none)
     if (!(r.s > 0.0 && r.s < INFINITY)) r.l = r.entropy = (double)kNan;
     return r;
@@ -325,7 +328,7 @@ __device__ __forceinline__ Slopes slopes_of(const RowEnd& e, const Goal& o, doub
     Slopes s;
     s.a0 = (float)(-f * (o.g - o.h * e.mean));
     s.a1 = (float)(-f * o.h * kLn2d);
-    s.gy = (float)(f * (o.g * e.se - (e.ey > 0.0 ? o.h * e.ey * (e.xy - e.mean) : 0.0)));
+    s.gy = (float)(f * (o.g * e.se - o.h * e.ey * e.over));
     return s;
 }
 

@@ -11,6 +11,7 @@ losses_ref.Row counts 2 y_v + 2 a term, 26 roundings, 4 for parts, and 3 more, w
 less; its bound of a 16-bit gradient counts 4 y_v, and here it is that of an fp32 gradient and
 the one rounding to the type.
 """
+import decimal
 import math
 
 import numpy as np
@@ -66,3 +67,37 @@ def test_sums_and_gradients(V, shift, dtype, tau):
             if dtype != "f32":
                 bound = bound + step * np.abs(want) * 1.01 + least
             within(got[r], want, bound, (r, h))
+
+
+def certain(z, tau):
+    """-l, H and the gradients of l and H at the first entry, the largest, in 60 digits; and
+    the largest distance in nats."""
+    with decimal.localcontext() as c:
+        c.prec = 60
+        D = decimal.Decimal
+        y = [(D(float(z[0])) - D(float(v))) / D(tau) for v in z[1:]]
+        e = [(-v).exp() for v in y]
+        se = sum(e)
+        s, ey = 1 + se, sum(a * b for a, b in zip(e, y))
+        return [float(v) for v in (s.ln(), s.ln() + ey / s, se / s / D(tau), -ey / (s * s) / D(tau), max(y))]
+
+
+@pytest.mark.parametrize("gap", [8, 20, 36, 40, 50, 60, 78])
+@pytest.mark.parametrize("V", [2, 9, 300, 40000])
+def test_nearly_certain_tokens_keep_their_digits(V, gap):
+    """Every term of l, H and their gradients at such a token has the same sign, so what they
+    are off by is relative: a term's 2 y + 2.03 and 26 roundings of sums as above; y and the
+    product in H's terms 2 more, a part's offset 4, the token's own exponential and the
+    rounding to fp32 4: U (2 y + 40)."""
+    rng = np.random.default_rng(V + gap)
+    one = dev(np.ones(1, np.float32))
+    for tau in (1.0, 0.25, *worst_temperatures()):
+        z = rng.normal(0, tau, (1, V)).astype(np.float32)
+        z[0, 0] = z[0, 1:].max() + gap * tau
+        x, tok = dev(z), dev(np.zeros(1, np.int32))
+        want = certain(z[0], tau)
+        l, H, g = P().hbsjd_logprob_rows(x, tok, temperature=tau, entropy=True, logprob_weight=one, grad=True)
+        h = P().hbsjd_logprob_rows(x, tok, temperature=tau, entropy_weight=one, grad=True)[2]
+        for got, w in zip((-l[0], H[0], g[0, 0], h[0, 0]), want):
+            # terms that fp32's exponentials drop: V of them below 2^-126, times 128 nats
+            assert abs(float(got) - w) <= 2.0 ** -24 * (2 * want[4] + 40) * abs(w) + V * 128 * 2.0 ** -126 / tau, tau
