@@ -460,6 +460,8 @@ def _matrix(t, what: str, like=None):
         raise ValueError(f"{what}: rows of {V} entries")
     if like is not None and (t.shape != like.shape or t.device != like.device):
         raise ValueError(f"{what}: expected shape {tuple(like.shape)} on {like.device}")
+    if rows == 0:   # whatever its strides
+        return 0, V, V
     ld, step = t.stride()
     if step != 1 and V > 1:
         raise ValueError(f"{what}: the entries of a row have to be adjacent")

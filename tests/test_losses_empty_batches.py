@@ -40,3 +40,17 @@ def test_empty_packed_batch(rows, grad):
     loss, g, s = P.hbsjd_preference_rows(x, tok, first=first, grad=grad)
     assert loss.shape == (0,) and s.shape == (0,)
     assert (g is not None and g.shape == x.shape and bool((g == 0).all())) if grad else g is None
+
+
+@pytest.mark.gpu
+def test_no_rows_of_any_strides():
+    """A matrix without rows has no entries that could lie apart."""
+    x = torch.empty_strided((0, 8), (1, 2), device="cuda")
+    f, i = torch.zeros(0, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert x.shape == (0, 8) and x.stride(1) != 1
+    assert P.hbsjd_logprob_rows(x, i, logprob_weight=f, grad=True)[2].shape == (0, 8)
+    assert P.hbsjd_logprob_rows(x, i, logprob_weight=f, grad=x)[2] is x
+    assert P.hbsjd_policy_rows(x, i, f)[1].shape == (0, 8)
+    loss, grad, s = P.hbsjd_preference_rows(x, i, pairs=2)
+    assert loss.shape == (2,) and s.tolist() == [0.0] * 4 and grad.shape == (0, 8)
+    assert P.hbsjd_top_logits_rows(x, 3)[0].shape == (0, 3)
